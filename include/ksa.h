@@ -314,6 +314,90 @@ int ksa_decode_summary_fwd(const ksa_params *params /*host*/, const void *q, con
                            const int64_t cache_strides[3], void *workspace, size_t workspace_bytes,
                            int32_t n_splits, void *stream);
 
+/* ---- paged cache: many new rows per sequence, bf16 or 8-bit floats ------------------------------------------- */
+
+/*
+ * A batch of augmented sequences (Eq. 1) whose K / V rows lie in pages of one pool.  A page is page_rows rows of every KV
+ * head.  Text index i of sequence b lies in slot i mod page_rows of page text_table[b, i div page_rows], summary ordinal u in slot
+ * u mod page_rows of page summary_table[b, u div page_rows].  Nothing else says where a row is: the two tables may name one page for
+ * several sequences (a shared prompt), and a page that only holds text behind the window (Eq. 3) may be given to other
+ * rows; its entry is then negative.  An entry outside [0, n_pages), and a row behind a table's last column, is no page: a row that
+ * goes there is not written, is read back as NaN, and makes the outputs of the rows that see it NaN.  Entries that no row of the call lies
+ * in or sees may hold anything.
+ *
+ * KSA_CACHE_FP8 holds a row of one KV head as 8-bit floats (e4m3: 4 significant bits, largest 448) times a power of two 2^e:
+ * e is the least integer in [-117, 119] with max |x| <= 448 * 2^e over the row's finite elements (119 if none is), every element is x / 2^e rounded
+ * to the nearest e4m3 number (ties to even; what lies beyond 448 * 2^119 = 2.98e38 becomes that), infinities and NaN become NaN.  k_exp and v_exp hold e + 127.  What a row stands for
+ * is zero or a normal bf16 number per element: reading it back and attending to it add no rounding.
+ */
+#define KSA_CACHE_BF16 0
+#define KSA_CACHE_FP8 1
+typedef struct ksa_paged_cache {
+    int32_t format;                 /* KSA_CACHE_*                                                                     */
+    int32_t page_rows;              /* rows per page: a power of two in [8, 1024]                                      */
+    int32_t n_pages;                /* pages in the pool                                                               */
+    int32_t text_pages;             /* columns of text_table                                                           */
+    int32_t summary_pages;          /* columns of summary_table; 0 only if n_summary is 0                              */
+    int32_t reserved;               /* 0                                                                               */
+    const int32_t *text_table;      /* device [batch, text_pages]                                                      */
+    const int32_t *summary_table;   /* device [batch, summary_pages]; may be NULL if n_summary is 0                    */
+    void *k, *v;                    /* device, bf16 or e4m3, [n_pages, Hkv, page_rows, d], last dim contiguous         */
+    uint8_t *k_exp, *v_exp;         /* device [n_pages, Hkv, page_rows] contiguous for KSA_CACHE_FP8, else NULL        */
+    int64_t strides[3];             /* of k and v: {page, head, row} in elements, multiples of 16 bytes; {0, 0, 0} = contiguous */
+} ksa_paged_cache;
+
+/*
+ * The calls below take a ragged batch of new rows, one behind the other in tensors of total_rows rows: rows
+ * [cu_rows[b], cu_rows[b + 1]) (device int32 [batch + 1], not decreasing, within [0, total_rows]) belong to sequence b and are
+ * its augmented rows start[b], start[b] + 1, ... (device int32 [batch]); a sequence may have none.  Rows of no sequence are
+ * left as they are.  A sequence with start[b] < 0, with rows behind those of params->n_text text tokens (the capacity), or
+ * whose two entries of cu_rows lie outside [0, total_rows] is out of place: ksa_paged_append skips it, the other calls set its rows to NaN.
+ * Nothing is allocated, cleared or waited for: all of them may be captured into a graph, and what lies in device memory (cu_rows,
+ * start, the tables) may change between replays.  total_rows = 0 is a no-op.
+ * kv_strides, q_strides, o_strides: {row, head} in elements, multiples of 8, the last dim contiguous; NULL = contiguous.
+ * Errors of all: INVALID_ARG (null or misaligned pointers: 16 bytes, 4 for int32 and fp32; bad strides or cache fields), UNSUPPORTED (2^31 and
+ * more (row, head) pairs; what ksa_params excludes), HIP.
+ */
+
+/* Columns that the tables need for the first n_rows augmented rows of a sequence. */
+int ksa_paged_pages(const ksa_params *params /*host*/, int32_t page_rows, int64_t n_rows, int64_t *text_pages /*host*/,
+                    int64_t *summary_pages /*host*/);
+
+/*
+ * ksa_paged_append: k_new, v_new (device bf16 [total_rows, Hkv, d]) go into the cache.  One call takes a step's token, a chunk
+ * of a prompt or all of it (start[b] = 0: the k, v of ksa_prefill_fwd), text and summary rows alike.  Rows without a page are skipped.  If two rows of a
+ * call go to one place, which of them is held afterwards is not said (and K may be the one's, V the other's).
+ */
+int ksa_paged_append(const ksa_params *params /*host*/, const ksa_paged_cache *cache /*host*/, const void *k_new, const void *v_new,
+                     const int64_t kv_strides[2], const int32_t *cu_rows, const int32_t *start, int64_t total_rows, void *stream);
+
+/* ksa_paged_read: the same rows back out of the cache, as bf16, into k, v (device [total_rows, Hkv, d]). */
+int ksa_paged_read(const ksa_params *params /*host*/, const ksa_paged_cache *cache /*host*/, void *k, void *v,
+                   const int64_t kv_strides[2], const int32_t *cu_rows, const int32_t *start, int64_t total_rows, void *stream);
+
+/* Bytes of device workspace ksa_paged_fwd needs for total_rows new rows, at most max_rows of one sequence, and this number of key splits
+ * (0 = library default); 0 also for arguments that make no sense. */
+size_t ksa_paged_workspace_bytes(const ksa_params *params /*host*/, int64_t total_rows, int64_t max_rows, int32_t n_splits);
+
+/*
+ * ksa_paged_fwd: the new rows attend to what they see (Eq. 3), their own K / V rows included, which must be in the cache.  One row
+ * per sequence is a decode step, of text or of a summary token; a few are drafted tokens checked in one pass; thousands are a
+ * chunk of a prompt.  What a row's outputs are does not depend on how the rows before it were dealt to calls, apart from rounding.
+ *   q, o: device bf16 [total_rows, Hq, d]; lse: device fp32 [total_rows, Hq] contiguous, natural-log sum-exp of the scaled
+ *   visible scores, or NULL.  o may be the memory of q (same strides).
+ *   max_rows: no sequence has more new rows; one that has is out of place.  It sizes the launch.
+ *   workspace: device, 16-byte aligned, at least ksa_paged_workspace_bytes(params, total_rows, max_rows, n_splits) bytes (NULL if that is 0),
+ *   needed until the work enqueued on `stream` has finished; calls that share one must be stream-ordered.
+ *   n_splits: spans that the keys of a sequence are cut into, each read by workgroups of its own; 0: the library chooses (by params->n_text,
+ *   the context that it must reckon with), else 1 .. 1024.
+ * Scores, maxima and sums are fp32; weights are rounded to bf16 for P V.  A row's outputs depend on nothing that it does not see:
+ * infinities and NaN elsewhere do not reach it.  No atomics.
+ * Errors also: WORKSPACE_TOO_SMALL.
+ */
+int ksa_paged_fwd(const ksa_params *params /*host*/, const ksa_paged_cache *cache /*host*/, const void *q, void *o, float *lse,
+                  const int64_t q_strides[2], const int64_t o_strides[2], const int32_t *cu_rows, const int32_t *start,
+                  int64_t total_rows, int64_t max_rows, void *workspace, size_t workspace_bytes, int32_t n_splits, void *stream);
+
 const char *ksa_status_string(int status);
 /* Static description of the build: tile sizes and the gfx target, e.g. for logs. */
 const char *ksa_build_info(void);

@@ -85,6 +85,11 @@ def lib():
         "ksa_decode_summary_fwd": (C.c_int, [pp, vp, vp, vp, vp, vp, vp, i64p, vp, C.c_size_t, C.c_int32, vp]),
         "ksa_cache_from_prefill": (C.c_int, [pp, C.c_int64, vp, vp, i64p, vp, vp, i64p, vp]),
         "ksa_cache_append": (C.c_int, [pp, C.c_int32, vp, vp, vp, vp, vp, i64p, vp]),
+        "ksa_paged_pages": (C.c_int, [pp, C.c_int32, C.c_int64, i64p, i64p]),
+        "ksa_paged_append": (C.c_int, [pp, vp, vp, vp, i64p, vp, vp, C.c_int64, vp]),
+        "ksa_paged_read": (C.c_int, [pp, vp, vp, vp, i64p, vp, vp, C.c_int64, vp]),
+        "ksa_paged_workspace_bytes": (C.c_size_t, [pp, C.c_int64, C.c_int64, C.c_int32]),
+        "ksa_paged_fwd": (C.c_int, [pp, vp, vp, vp, vp, i64p, i64p, vp, vp, C.c_int64, C.c_int64, vp, C.c_size_t, C.c_int32, vp]),
         "ksa_status_string": (C.c_char_p, [C.c_int]),
         "ksa_build_info": (C.c_char_p, []),
     }
@@ -101,7 +106,8 @@ EXPORTED_SYMBOLS = ("ksa_augmented_rows", "ksa_build_layout", "ksa_layout_destro
                     "ksa_prefill_bwd_workspace_bytes", "ksa_prefill_bwd", "ksa_cache_geometry", "ksa_cache_text_row",
                     "ksa_cache_summary_row", "ksa_decode_ranges", "ksa_decode_workspace_bytes",
                     "ksa_decode_fwd", "ksa_decode_fwd_static", "ksa_decode_summary_ranges", "ksa_decode_summary_fwd", "ksa_cache_from_prefill",
-                    "ksa_cache_append", "ksa_status_string", "ksa_build_info")
+                    "ksa_cache_append", "ksa_paged_pages", "ksa_paged_append", "ksa_paged_read", "ksa_paged_workspace_bytes", "ksa_paged_fwd",
+                    "ksa_status_string", "ksa_build_info")
 
 
 def status_string(status: int) -> str:
@@ -520,6 +526,160 @@ def _append_checks(params: ksa_params, k_new, v_new, pos, k_cache, v_cache):
             not k_new.is_contiguous() or not v_new.is_contiguous() or pos.shape[0] != params.batch:
         raise ValueError("k_new / v_new / pos shape does not match params")
     return _strides3(k_cache)
+
+
+KSA_CACHE_BF16, KSA_CACHE_FP8 = 0, 1
+
+
+class ksa_paged_cache(C.Structure):
+    _fields_ = [("format", C.c_int32), ("page_rows", C.c_int32), ("n_pages", C.c_int32), ("text_pages", C.c_int32),
+                ("summary_pages", C.c_int32), ("reserved", C.c_int32), ("text_table", C.c_void_p), ("summary_table", C.c_void_p),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p), ("strides", C.c_int64 * 3)]
+
+
+class PagedCache:
+    """A batch of sequences whose K / V rows lie in the pages of one pool (struct ksa_paged_cache); holds its tensors.
+
+    k, v: [n_pages, Hkv, page_rows, d] on the GPU, bfloat16, or float8_e4m3fn with k_exp, v_exp uint8 [n_pages, Hkv, page_rows].
+    text_table, summary_table: int32 [batch, columns], contiguous; their contents may change from call to call.
+    """
+
+    def __init__(self, params: ksa_params, k, v, text_table, summary_table=None, k_exp=None, v_exp=None):
+        import torch
+        f8 = k.dtype is torch.float8_e4m3fn
+        for t, name in ((k, "k"), (v, "v")):
+            _require(t, name, torch.float8_e4m3fn if f8 else torch.bfloat16, 4)
+        n_pages, heads, rows, d = k.shape
+        if (heads, d) != (params.n_kv_heads, params.head_dim) or k.shape != v.shape or not _same_strides(k, v):
+            raise ValueError(f"k / v shape must be [n_pages, {params.n_kv_heads}, page_rows, {params.head_dim}], with the same strides")
+        if f8 != (k_exp is not None) or f8 != (v_exp is not None):
+            raise ValueError("k_exp and v_exp belong to a float8_e4m3fn cache, and to no other")
+        for t, name in ((k_exp, "k_exp"), (v_exp, "v_exp")) if f8 else ():
+            _require(t, name, torch.uint8, 3)
+            if tuple(t.shape) != (n_pages, heads, rows) or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous {(n_pages, heads, rows)}")
+        if params.n_summary > 0 and summary_table is None:
+            raise ValueError("summary_table is missing")
+        for t, name in ((text_table, "text_table"), (summary_table, "summary_table")):
+            if t is not None:
+                _require(t, name, torch.int32, 2)
+                if t.shape[0] != params.batch or not t.is_contiguous():
+                    raise ValueError(f"{name} must be contiguous with {params.batch} rows")
+        tensors = [t for t in (k, v, text_table, summary_table, k_exp, v_exp) if t is not None]
+        if any(t.device != k.device for t in tensors):
+            raise ValueError("the cache's tensors lie on different devices")
+        self.params, self.device = params, k.device
+        self.k, self.v, self.text_table, self.summary_table, self.k_exp, self.v_exp = k, v, text_table, summary_table, k_exp, v_exp
+        ptr = [t.data_ptr() if t is not None else None for t in (text_table, summary_table, k, v, k_exp, v_exp)]
+        self.struct = ksa_paged_cache(KSA_CACHE_FP8 if f8 else KSA_CACHE_BF16, rows, n_pages, text_table.shape[1],
+                                      summary_table.shape[1] if summary_table is not None else 0, 0, *ptr, _strides_of(k))
+
+    @property
+    def page_rows(self) -> int:
+        return self.struct.page_rows
+
+
+def _strides_of(t):
+    """Strides for the library: those of dimensions of size 1, which may be anything, as in a contiguous tensor."""
+    strides, size = [], t.stride(-1) * t.shape[-1]
+    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        strides.insert(0, size if n == 1 else s)
+        size = strides[0] * n
+    return (C.c_int64 * len(strides))(*strides)
+
+
+def paged_pages(params: ksa_params, page_rows: int, n_rows: int) -> Tuple[int, int]:
+    """Columns that text_table and summary_table need for the first n_rows augmented rows of a sequence."""
+    t, s = C.c_int64(), C.c_int64()
+    _check(lib().ksa_paged_pages(C.byref(params), page_rows, n_rows, C.byref(t), C.byref(s)), "ksa_paged_pages")
+    return t.value, s.value
+
+
+def paged_workspace_bytes(cache: PagedCache, total_rows: int, max_rows: int, n_splits: int = 0) -> int:
+    return int(lib().ksa_paged_workspace_bytes(C.byref(cache.params), total_rows, max_rows, n_splits))
+
+
+def _rows_of_call(cache: PagedCache, tensors, heads, cu_rows, start):
+    """Checks the tensors [rows, heads, d] and the batch of a call."""
+    import torch
+    d = cache.params.head_dim
+    for t, name in tensors:
+        _require(t, name, torch.bfloat16, 3)
+        if tuple(t.shape) != (tensors[0][0].shape[0], heads, d):
+            raise ValueError(f"{name}: expected [rows, {heads}, {d}], got {tuple(t.shape)}")
+    for t, name, n in ((cu_rows, "cu_rows", cache.params.batch + 1), (start, "start", cache.params.batch)):
+        _require(t, name, torch.int32, 1)
+        if t.shape[0] != n:
+            raise ValueError(f"{name} must have {n} elements")
+    if any(t.device != cache.device for t, _ in tensors) or cu_rows.device != cache.device or start.device != cache.device:
+        raise ValueError("tensors lie on another device than the cache")
+
+
+def _paged(cache: PagedCache, name, stream, *args):
+    """The call, on the cache's device: on `stream`, or on that device's current one."""
+    from torch import _C
+    if stream is not None and stream.device != cache.device:
+        raise ValueError("stream belongs to another device than the cache")
+    here, there = _C._cuda_getDevice(), cache.device.index
+    raw = stream.cuda_stream if stream is not None else _C._cuda_getCurrentRawStream(there)
+    if here != there:
+        _C._cuda_setDevice(there)
+    try:
+        rc = getattr(lib(), name)(C.byref(cache.params), C.byref(cache.struct), *args, raw)
+    finally:
+        if here != there:
+            _C._cuda_setDevice(here)
+    if rc:
+        _check(rc, name)
+
+
+def ksa_paged_append(cache: PagedCache, k_new, v_new, cu_rows, start, stream=None):
+    """k_new, v_new [rows, Hkv, d] bf16: rows [cu_rows[b], cu_rows[b + 1]) become sequence b's augmented rows from start[b] on.
+    cu_rows int32 [batch + 1] and start int32 [batch] lie on the GPU."""
+    _rows_of_call(cache, ((k_new, "k_new"), (v_new, "v_new")), cache.params.n_kv_heads, cu_rows, start)
+    if not _same_strides(k_new, v_new):
+        raise ValueError("k_new and v_new must have the same strides")
+    _paged(cache, "ksa_paged_append", stream, k_new.data_ptr(), v_new.data_ptr(), _strides_of(k_new), cu_rows.data_ptr(), start.data_ptr(),
+           k_new.shape[0])
+
+
+def ksa_paged_read(cache: PagedCache, cu_rows, start, total_rows: int, k=None, v=None, stream=None):
+    """The rows that ksa_paged_append with these cu_rows and start would write -> k, v [total_rows, Hkv, d] bf16."""
+    import torch
+    shape = (total_rows, cache.params.n_kv_heads, cache.params.head_dim)
+    k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if k is None else k
+    v = torch.empty_like(k) if v is None else v
+    _rows_of_call(cache, ((k, "k"), (v, "v")), shape[1], cu_rows, start)
+    if k.shape[0] != total_rows or not _same_strides(k, v):
+        raise ValueError(f"k and v must be {shape}, with the same strides")
+    _paged(cache, "ksa_paged_read", stream, k.data_ptr(), v.data_ptr(), _strides_of(k), cu_rows.data_ptr(), start.data_ptr(), total_rows)
+    return k, v
+
+
+def ksa_paged_fwd(cache: PagedCache, q, cu_rows, start, max_rows: Optional[int] = None, o=None, lse=None, return_lse=True, workspace=None,
+                  n_splits: int = 0, stream=None):
+    """q [rows, Hq, d] bf16, the queries of the rows that ksa_paged_append wrote -> o like q, lse [rows, Hq] fp32.
+    max_rows: the largest number of rows of a sequence (all of them if omitted); workspace: uint8, at least
+    paged_workspace_bytes(cache, rows, max_rows, n_splits) bytes (allocated here if omitted)."""
+    import torch
+    rows, heads = q.shape[0], cache.params.n_q_heads
+    max_rows = max(rows, 1) if max_rows is None else max_rows
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _rows_of_call(cache, ((q, "q"), (o, "o")), heads, cu_rows, start)
+    if lse is None and return_lse:
+        lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device)
+    if lse is not None:
+        _require(lse, "lse", torch.float32, 2)
+        if tuple(lse.shape) != (rows, heads) or not lse.is_contiguous() or lse.device != cache.device:
+            raise ValueError(f"lse must be contiguous {(rows, heads)} on the cache's device")
+    if workspace is None:
+        workspace = torch.empty(paged_workspace_bytes(cache, rows, max_rows, n_splits), dtype=torch.uint8, device=q.device)
+    if workspace.device != cache.device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
+    _paged(cache, "ksa_paged_fwd", stream, q.data_ptr(), o.data_ptr(), lse.data_ptr() if lse is not None else None, _strides_of(q), _strides_of(o),
+           cu_rows.data_ptr(), start.data_ptr(), rows, max_rows, workspace.data_ptr(), workspace.numel(), n_splits)
+    return o, lse
 
 
 def pack_cache(params: ksa_params, k_sum, v_sum, k_txt, v_txt, txt_base: int):

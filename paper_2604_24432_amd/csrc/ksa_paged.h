@@ -1,0 +1,87 @@
+// The paged cache's launches: what the argument checks hand to the kernels, and the device-side pieces that the kernels share.
+#ifndef KSA_PAGED_H_
+#define KSA_PAGED_H_
+
+#include "ksa.h"
+
+// A checked call on the paged cache.  Strides in bytes, defaults filled in.
+struct KsaPagedCall {
+    ksa_params p;
+    ksa_paged_cache cache;
+    int64_t cache_strides[3];     // {page, head, row}
+    int32_t page_shift;
+    int32_t aug_len;              // augmented rows of a sequence of params.n_text text tokens
+    const int32_t *cu_rows, *start;
+    int32_t total_rows;
+};
+
+// rows in (append) or out (read): k, v [total_rows, Hkv, d] bf16
+struct KsaPagedMove {
+    KsaPagedCall call;
+    void *k, *v;
+    int64_t strides[2];           // {row, head}
+};
+int ksa_launch_paged_append(const KsaPagedMove &a, void *stream);
+int ksa_launch_paged_read(const KsaPagedMove &a, void *stream);
+
+// How the attention of a call is dealt to workgroups.
+struct KsaPagedPlan {
+    int32_t columns;              // 16 or 32: the kernel for few rows, with so many (row, query head) pairs at most; 0: the one for many
+    int32_t n_splits;             // spans of the keys
+    int32_t slots;                // many rows: query tiles of all sequences, none less
+};
+// Query tiles of the kernel for many rows hold so many (row, query head) pairs.
+#define KSA_PAGED_PAIRS 128
+// Floats of a span's record for one (row, query head): the output, then maximum and sum (padded to 16 bytes)
+inline int64_t ksa_paged_record(int32_t head_dim) { return head_dim + 4; }
+
+struct KsaPagedFwd {
+    KsaPagedCall call;
+    KsaPagedPlan plan;
+    const void *q;
+    void *o;
+    float *lse, *workspace;
+    int64_t q_strides[2], o_strides[2];   // {row, head}
+    int32_t max_rows;
+};
+int ksa_launch_paged_fwd(const KsaPagedFwd &a, void *stream);
+
+#ifdef __HIPCC__
+#include "ksa_device.h"
+#include "ksa_paged_index.h"
+
+namespace {
+
+inline PagedRows paged_rows(const KsaPagedCall &L) {
+    PagedRows a;
+    a.text_table = L.cache.text_table, a.sum_table = L.cache.summary_table;
+    a.text_cols = L.cache.text_pages, a.sum_cols = L.p.n_summary > 0 ? L.cache.summary_pages : 0;
+    a.n_pages = L.cache.n_pages, a.shift = L.page_shift;
+    a.cu = L.cu_rows, a.start = L.start, a.batch = L.p.batch, a.total = L.total_rows, a.aug_len = L.aug_len;
+    a.c = L.p.chunk_len, a.m = L.p.n_summary, a.C = L.p.window_chunks, a.self_only = (L.p.flags & KSA_FLAG_SUMMARY_SELF_ONLY) ? 1 : 0;
+    a.by_w = ksa_divisor(a.c + a.m), a.by_c = ksa_divisor(a.c), a.by_m = ksa_divisor(a.m > 0 ? a.m : 1);
+    return a;
+}
+
+// The sequence of a packed row: so many end at or in front of it (cu_rows does not decrease); a.batch if none is left.  The row is the same
+// for all lanes of the wave.
+__device__ __forceinline__ int sequence_of(const PagedRows &a, int row) {
+    const int lane = threadIdx.x & 63;
+    for (int b = 0; b < a.batch; b += 64) {
+        const uint64_t ended = __builtin_amdgcn_ballot_w64(b + lane < a.batch && a.cu[min(b + lane, a.batch - 1) + 1] <= row);
+        if (ended != ~(uint64_t)0) return b + __builtin_popcountll(ended);
+    }
+    return a.batch;
+}
+
+// Four e4m3 numbers times `scale`, a power of two, as bf16.
+__device__ __forceinline__ u32x2 unpack_fp8(unsigned x, float scale) {
+    return {__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false)),
+            __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true))};
+}
+__device__ __forceinline__ float power_of_two(int biased) { return __builtin_bit_cast(float, biased << 23); }
+
+}  // namespace
+#endif
+
+#endif

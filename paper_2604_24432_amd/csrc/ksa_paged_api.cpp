@@ -1,0 +1,164 @@
+// C-ABI entry points of the paged cache.  Every argument check happens before the first HIP call.
+#include <algorithm>
+
+#include "ksa_internal.h"
+#include "ksa_paged.h"
+
+namespace {
+
+bool aligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+int64_t augmented(const ksa_params *p) {
+    return (int64_t)(p->n_text / p->chunk_len) * (p->chunk_len + p->n_summary) + p->n_text % p->chunk_len;
+}
+
+int check_sizes(const ksa_params *p, int64_t total_rows) {
+    const int rc = ksa_validate_params(p);
+    if (rc != KSA_OK) return rc;
+    if (total_rows < 0) return KSA_ERR_INVALID_ARG;
+    if (total_rows >= ((int64_t)1 << 31) / p->n_q_heads) return KSA_ERR_UNSUPPORTED;   // (row, head) pairs are int32 on the device
+    return KSA_OK;
+}
+
+// The cache and the batch of a call, checked, with defaults filled in.
+int check_call(KsaPagedCall &c, const ksa_params *p, const ksa_paged_cache *cache, const int32_t *cu_rows, const int32_t *start, int64_t total_rows) {
+    const int rc = check_sizes(p, total_rows);
+    if (rc != KSA_OK) return rc;
+    if (!cache || !cu_rows || !start || !aligned(cu_rows, 4) || !aligned(start, 4)) return KSA_ERR_INVALID_ARG;
+    const bool f8 = cache->format == KSA_CACHE_FP8;
+    if ((!f8 && cache->format != KSA_CACHE_BF16) || cache->reserved != 0) return KSA_ERR_INVALID_ARG;
+    const int32_t rows = cache->page_rows;
+    if (rows < 8 || rows > 1024 || (rows & (rows - 1)) || cache->n_pages <= 0) return KSA_ERR_INVALID_ARG;
+    if (cache->text_pages <= 0 || !cache->text_table || !aligned(cache->text_table, 4)) return KSA_ERR_INVALID_ARG;
+    if (p->n_summary > 0 && (cache->summary_pages <= 0 || !cache->summary_table)) return KSA_ERR_INVALID_ARG;
+    if (cache->summary_pages < 0 || !aligned(cache->summary_table, 4)) return KSA_ERR_INVALID_ARG;
+    if (!cache->k || !cache->v || !aligned(cache->k, 16) || !aligned(cache->v, 16)) return KSA_ERR_INVALID_ARG;
+    if (f8 != (cache->k_exp != nullptr) || f8 != (cache->v_exp != nullptr)) return KSA_ERR_INVALID_ARG;
+    const int64_t *s = cache->strides, size = f8 ? 1 : 2;
+    if (s[0] == 0 && s[1] == 0 && s[2] == 0) {
+        c.cache_strides[2] = p->head_dim * size;
+        c.cache_strides[1] = rows * c.cache_strides[2];
+        c.cache_strides[0] = p->n_kv_heads * c.cache_strides[1];
+    } else {
+        for (int x = 0; x < 3; ++x) {
+            if (s[x] <= 0 || s[x] > INT64_MAX / 2 || (s[x] * size) % 16 != 0) return KSA_ERR_INVALID_ARG;
+            c.cache_strides[x] = s[x] * size;
+        }
+    }
+    c.p = *p, c.cache = *cache;
+    if (c.p.softmax_scale <= 0.f) c.p.softmax_scale = 1.0f / __builtin_sqrtf((float)p->head_dim);
+    c.page_shift = __builtin_ctz((unsigned)rows);
+    c.aug_len = (int32_t)augmented(p);
+    c.cu_rows = cu_rows, c.start = start, c.total_rows = (int32_t)total_rows;
+    return KSA_OK;
+}
+
+// {row, head} strides in elements of a [rows, heads, head_dim] bf16 tensor
+int check_strides(int64_t out[2], const int64_t *given, int32_t heads, int32_t head_dim) {
+    out[0] = given ? given[0] : (int64_t)heads * head_dim, out[1] = given ? given[1] : head_dim;
+    return out[0] > 0 && out[1] > 0 && out[0] % 8 == 0 && out[1] % 8 == 0 ? KSA_OK : KSA_ERR_INVALID_ARG;
+}
+
+// Keys that a sequence's rows see together, none less: the summaries, the text of the window and of the new rows.
+int64_t most_keys(const ksa_params *p, int64_t max_rows) {
+    const int64_t text = std::min<int64_t>(p->n_text, (int64_t)p->window_chunks * p->chunk_len + p->chunk_len + max_rows);
+    return (int64_t)(p->n_text / p->chunk_len) * p->n_summary + text;
+}
+
+KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_rows, int32_t n_splits) {
+    const int32_t group = p->n_q_heads / p->n_kv_heads;
+    KsaPagedPlan plan = {0, 1, 0};
+    const int64_t pairs = max_rows * group, keys = most_keys(p, max_rows);
+    int64_t units, want, least;   // workgroups of one span; how many are wanted; keys of a span
+    if (pairs <= 32) {
+        plan.columns = pairs <= 16 ? 16 : 32;
+        units = (int64_t)p->batch * p->n_kv_heads, want = 1024, least = 256;
+    } else {
+        // every sequence ends one tile of text and one of summaries before it is full
+        plan.slots = (int32_t)((total_rows * group) / KSA_PAGED_PAIRS + (p->n_summary > 0 ? 2 : 1) * (int64_t)p->batch);
+        units = (int64_t)plan.slots * p->n_kv_heads, want = 512, least = 512;
+    }
+    plan.n_splits = n_splits;
+    if (n_splits == 0) plan.n_splits = (int32_t)std::max<int64_t>(1, std::min({want / units, keys / least, (int64_t)64}));
+    return plan;
+}
+
+bool bad_fwd(int64_t max_rows, int32_t n_splits) { return max_rows <= 0 || n_splits < 0 || n_splits > 1024; }
+
+// more workgroups than a grid may have, or more records than bytes of a workspace can be counted
+bool too_large(const ksa_params *p, const KsaPagedPlan &plan) { return (int64_t)plan.slots * plan.n_splits * p->n_kv_heads >= (int64_t)1 << 31; }
+
+size_t workspace_of(const ksa_params *p, int64_t total_rows, const KsaPagedPlan &plan) {
+    return plan.n_splits == 1 ? 0 : (size_t)total_rows * p->n_q_heads * plan.n_splits * ksa_paged_record(p->head_dim) * sizeof(float);
+}
+
+int move_call(KsaPagedMove &a, const ksa_params *p, const ksa_paged_cache *cache, const void *k, const void *v, const int64_t *strides,
+              const int32_t *cu_rows, const int32_t *start, int64_t total_rows) {
+    const int rc = check_call(a.call, p, cache, cu_rows, start, total_rows);
+    if (rc != KSA_OK) return rc;
+    if (total_rows > 0 && (!k || !v)) return KSA_ERR_INVALID_ARG;
+    if (!aligned(k, 16) || !aligned(v, 16)) return KSA_ERR_INVALID_ARG;
+    return check_strides(a.strides, strides, p->n_kv_heads, p->head_dim);
+}
+
+}  // namespace
+
+extern "C" {
+
+int ksa_paged_pages(const ksa_params *p, int32_t page_rows, int64_t n_rows, int64_t *text_pages, int64_t *summary_pages) {
+    const int rc = ksa_validate_params(p);
+    if (rc != KSA_OK) return rc;
+    if (page_rows < 8 || page_rows > 1024 || (page_rows & (page_rows - 1)) || n_rows < 0) return KSA_ERR_INVALID_ARG;
+    if (n_rows > augmented(p)) return KSA_ERR_OUT_OF_RANGE;
+    const int64_t w = p->chunk_len + p->n_summary, text = n_rows / w * p->chunk_len + std::min<int64_t>(n_rows % w, p->chunk_len);
+    if (text_pages) *text_pages = (text + page_rows - 1) / page_rows;
+    if (summary_pages) *summary_pages = (n_rows - text + page_rows - 1) / page_rows;
+    return KSA_OK;
+}
+
+int ksa_paged_append(const ksa_params *p, const ksa_paged_cache *cache, const void *k_new, const void *v_new, const int64_t kv_strides[2],
+                     const int32_t *cu_rows, const int32_t *start, int64_t total_rows, void *stream) {
+    KsaPagedMove a;
+    const int rc = move_call(a, p, cache, k_new, v_new, kv_strides, cu_rows, start, total_rows);
+    if (rc != KSA_OK || total_rows == 0) return rc;
+    a.k = const_cast<void *>(k_new), a.v = const_cast<void *>(v_new);   // (read only)
+    return ksa_launch_paged_append(a, stream);
+}
+
+int ksa_paged_read(const ksa_params *p, const ksa_paged_cache *cache, void *k, void *v, const int64_t kv_strides[2], const int32_t *cu_rows,
+                   const int32_t *start, int64_t total_rows, void *stream) {
+    KsaPagedMove a;
+    const int rc = move_call(a, p, cache, k, v, kv_strides, cu_rows, start, total_rows);
+    if (rc != KSA_OK || total_rows == 0) return rc;
+    a.k = k, a.v = v;
+    return ksa_launch_paged_read(a, stream);
+}
+
+size_t ksa_paged_workspace_bytes(const ksa_params *p, int64_t total_rows, int64_t max_rows, int32_t n_splits) {
+    if (check_sizes(p, total_rows) != KSA_OK || bad_fwd(max_rows, n_splits) || total_rows == 0) return 0;
+    return workspace_of(p, total_rows, plan_paged(p, total_rows, std::min(max_rows, total_rows), n_splits));
+}
+
+int ksa_paged_fwd(const ksa_params *p, const ksa_paged_cache *cache, const void *q, void *o, float *lse, const int64_t q_strides[2],
+                  const int64_t o_strides[2], const int32_t *cu_rows, const int32_t *start, int64_t total_rows, int64_t max_rows,
+                  void *workspace, size_t workspace_bytes, int32_t n_splits, void *stream) {
+    KsaPagedFwd a;
+    int rc = check_call(a.call, p, cache, cu_rows, start, total_rows);
+    if (rc != KSA_OK) return rc;
+    if (bad_fwd(max_rows, n_splits)) return KSA_ERR_INVALID_ARG;
+    if (total_rows > 0 && (!q || !o)) return KSA_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(o, 16) || !aligned(lse, 4) || !aligned(workspace, 16)) return KSA_ERR_INVALID_ARG;
+    if ((rc = check_strides(a.q_strides, q_strides, p->n_q_heads, p->head_dim)) != KSA_OK) return rc;
+    if ((rc = check_strides(a.o_strides, o_strides, p->n_q_heads, p->head_dim)) != KSA_OK) return rc;
+    if (total_rows == 0) return KSA_OK;
+    a.max_rows = (int32_t)std::min(max_rows, total_rows);
+    a.plan = plan_paged(p, total_rows, a.max_rows, n_splits);
+    if (too_large(p, a.plan)) return KSA_ERR_UNSUPPORTED;
+    const size_t need = workspace_of(p, total_rows, a.plan);
+    if (need > 0 && !workspace) return KSA_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return KSA_ERR_WORKSPACE_TOO_SMALL;
+    a.q = q, a.o = o, a.lse = lse, a.workspace = static_cast<float *>(workspace);
+    return ksa_launch_paged_fwd(a, stream);
+}
+
+}  // extern "C"
