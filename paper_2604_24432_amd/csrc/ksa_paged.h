@@ -28,10 +28,9 @@ int ksa_launch_paged_read(const KsaPagedMove &a, void *stream);
 struct KsaPagedPlan {
     int32_t columns;              // 16 or 32: the kernel for few rows, with so many (row, query head) pairs at most; 0: the one for many
     int32_t n_splits;             // spans of the keys
-    int32_t slots;                // many rows: query tiles of all sequences, none less
+    int32_t pairs;                // many rows: (row, query head) pairs of a query tile, 128 or 256
+    int32_t slots;                // ... and query tiles of all sequences, none less
 };
-// Query tiles of the kernel for many rows hold so many (row, query head) pairs.
-#define KSA_PAGED_PAIRS 128
 // Floats of a span's record for one (row, query head): the output, then maximum and sum (padded to 16 bytes)
 inline int64_t ksa_paged_record(int32_t head_dim) { return head_dim + 4; }
 

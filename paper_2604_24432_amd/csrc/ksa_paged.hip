@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 #include "ksa_paged.h"
 
@@ -178,10 +179,10 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void ksa_paged_few_kernel(const Fwd
 
     const int step = FEW_WAVES * BLOCK;
     int x = v0 + wave * BLOCK;
-    Spot next = spot_of(a.rows, b, key_at(keys, min(x + (lane & 31), keys.n - 1)));
+    Entry next = entry_of(a.rows, b, key_at(keys, min(x + (lane & 31), keys.n - 1)));
     for (; x < v1; x += step) {
-        const Spot spot = next;
-        next = spot_of(a.rows, b, key_at(keys, min(x + step + (lane & 31), keys.n - 1)));
+        const Spot spot = spot_of(a.rows, next);
+        next = entry_of(a.rows, b, key_at(keys, min(x + step + (lane & 31), keys.n - 1)));
         const int64_t off = spot_bytes(a, spot);
         const unsigned lost = (unsigned)__builtin_amdgcn_ballot_w64(spot.page < 0);   // keys without a page
         int ke = 0, ve = 0;
@@ -246,7 +247,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void ksa_paged_few_kernel(const Fwd
                 s[e] = acc[e / 4][cb][e % 4] * a.score_scale;
                 if (!whole) {
                     const int key = (e / 4) * 16 + grp * 4 + e % 4;
-                    s[e] = !seen[cb].sees(x + key) ? -INFINITY : (lost >> key) & 1 ? __builtin_nanf("") : s[e];
+                    const float lost_or_not = (lost >> key) & 1 ? __builtin_nanf("") : s[e];
+                    s[e] = seen[cb].sees(x + key) ? lost_or_not : -INFINITY;
                 }
                 mx = fmaxf(mx, s[e]);
             }
@@ -275,6 +277,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void ksa_paged_few_kernel(const Fwd
             for (int cb = 0; cb < CB; ++cb) o[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p[cb], o[cb][db], 0, 0, 0);
         }
         if (odd) {
+#pragma unroll 1
             for (int key = 0; key < BLOCK; ++key) {
                 const Spot at = {__builtin_amdgcn_readlane(spot.page, key), __builtin_amdgcn_readlane(spot.slot, key)};
 #pragma unroll
@@ -337,26 +340,45 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void ksa_paged_few_kernel(const Fwd
 
 // ---- many rows ----------------------------------------------------------------------------------------------------------
 
-constexpr int NW = 4, BN = 64, RW = BN / NW;   // waves; keys of a tile; rows of it that a wave fetches
-static_assert(KSA_PAGED_PAIRS == NW * 32, "32 pairs per wave");
+constexpr int BN = 64;   // keys of a tile
+// A row's weights go by a reference that is one of its scores, not the largest: no weight is too small to count, and the sum of 16 of them is
+// looked at instead of their scores.  Above this a new reference is taken and the 16 are worked out again.
+constexpr float HIGH = 1048576.f;
+#define KSA_FENCE() __builtin_amdgcn_sched_barrier(0)
 
+// Bytes from one row of a tile to the next in LDS: the 16 rows of a phase of the plain reads of K, 16 bytes each, and the 4 rows of one of the
+// transposing reads of V, 64 bytes each, lie in different banks, and every address is a base plus a constant.
 template <int D>
-__device__ __forceinline__ int k_swz(int row) { return D == 64 ? (row >> 1) & 7 : row & (D / 8 - 1); }
-template <int D>
-__device__ __forceinline__ int v_swz(int row) { return D == 64 ? (row & 2) << 1 : ((row & 3) << 2) & (D / 8 - 1); }
+struct TileRow {
+    static constexpr int K = D * 2 + 16, V = D * 2 + 64;
+};
 
-// What a workgroup works on: pairs [first, first + 128) of sequence b's new text rows (or summary rows), p = row * group + head.
+// Bytes of an 8-bit word (halves of a word of bf16) that are no numbers become zero; whether there were any.
+template <bool F8>
+__device__ __forceinline__ bool take_out_raw(u32x4 &x) {
+    if constexpr (!F8) return take_out(x);
+    unsigned any = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const unsigned hit = ((x[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // (0x7f and 0xff are the NaNs)
+        any |= hit, x[e] &= ~((hit >> 7) * 0xffu);
+    }
+    return any != 0;
+}
+
+// What a workgroup works on: pairs [first, first + PAIRS) of sequence b's new text rows (or summary rows), p = row * group + head.
 struct Tile {
     int b, first;
     bool text;
     NewRows seq;
     int text0, n_text, n_sum;   // first new text row's index; how many new rows of either kind
 };
+template <int PAIRS>
 __device__ __forceinline__ Tile tile_of(const FwdArgs &a, int slot) {
     const int lane = threadIdx.x & 63;
     Tile t;
     t.b = -1;
-    auto tiles = [&](int rows) { return (int)(((int64_t)rows * a.group + KSA_PAGED_PAIRS - 1) / KSA_PAGED_PAIRS); };
+    auto tiles = [&](int rows) { return (int)(((int64_t)rows * a.group + PAIRS - 1) / PAIRS); };
     int before = 0;
     for (int base = 0; base < a.rows.batch; base += 64) {
         // every lane a sequence; its tiles, and those of the lanes up to it
@@ -378,7 +400,7 @@ __device__ __forceinline__ Tile tile_of(const FwdArgs &a, int slot) {
             const int in = slot - get(upto - mine), split_at = get(of_text);
             t.b = base + at;
             t.text = in < split_at;
-            t.first = (t.text ? in : in - split_at) * KSA_PAGED_PAIRS;
+            t.first = (t.text ? in : in - split_at) * PAIRS;
             t.seq = {get(s.first), get(s.n), get(s.start), get(s.ok ? 1 : 0) != 0};
             t.text0 = get(t0), t.n_text = get(n_t), t.n_sum = t.seq.n - t.n_text;
             return t;
@@ -388,29 +410,33 @@ __device__ __forceinline__ Tile tile_of(const FwdArgs &a, int slot) {
     return t;
 }
 
-template <int D, bool F8>
+// A step works on one tile of keys in two halves of 32.  What a half does: the scores of its keys, the weights of the half before, and the
+// product with V of the half before that, so that the matrix unit's and the vector unit's work do not wait for each other.
+// NW waves, 32 pairs each.
+template <int D, bool F8, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArgs a) {
-    constexpr int KS = D / 16, DB = D / 32, ES = F8 ? 1 : 2;
-    constexpr int LPR = D * ES / 16, RPI = 64 / LPR, NI = RW / RPI;   // lanes per row, rows per load, loads per wave and tensor
-    constexpr int BYTES = BN * D * 2;
+    constexpr int KS = D / 16, DB = D / 32, ES = F8 ? 1 : 2, PAIRS = NW * 32;
+    constexpr int RW = BN / NW;                                       // rows of a tile that a wave fetches
+    constexpr int LPR = D * ES / 16, RPI = 64 / LPR < RW ? 64 / LPR : RW, NI = RW / RPI;   // lanes per row, rows per load, loads per wave and tensor
+    constexpr int KROW = TileRow<D>::K, VROW = TileRow<D>::V, K_BYTES = BN * KROW, V_BYTES = BN * VROW;
+    constexpr int STAGE_ROW = D * 2 + 16;
     static_assert(RW % RPI == 0 && NI >= 1, "a wave's rows are whole loads");
-    __shared__ __align__(16) unsigned char lds[4 * BYTES];   // two buffers of K, then V
-    __shared__ uint64_t sh_lost[2];                          // tile's keys without a page
-    __shared__ int sh_odd[2][NW];                            // elements of V were taken out
+    static_assert(NW * 32 * STAGE_ROW <= 2 * (K_BYTES + V_BYTES), "the results pass through the tiles' memory");
+    __shared__ __align__(16) unsigned char lds[2 * (K_BYTES + V_BYTES)];   // two buffers of K, two of V
+    __shared__ __align__(16) unsigned sh_state[2][NW];   // of the K tile: which of a wave's rows have no page; bit 31: of the V tile before: elements were taken out
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 31, h = lane >> 5;
     // KV heads fastest: with a multiple of 8 of them the tiles of one share an L2
     const int rest = ksa_div(blockIdx.x, a.by_heads), hkv = blockIdx.x - rest * a.n_kv_heads;
     const int slot = ksa_div(rest, a.by_splits), split = rest - slot * a.n_splits;
-    const Tile tile = tile_of(a, slot);
+    const Tile tile = tile_of<PAIRS>(a, slot);
     if (tile.b < 0) return;
     const NewRows seq = tile.seq;
     const int n_rows = tile.text ? tile.n_text : tile.n_sum;
-    const int64_t all_pairs = (int64_t)n_rows * a.group;
-    const int n_pairs = (int)min((int64_t)KSA_PAGED_PAIRS, all_pairs - tile.first);
+    const int n_pairs = (int)min((int64_t)PAIRS, (int64_t)n_rows * a.group - tile.first);
     if (!seq.ok) {
-        if (a.n_splits > 1) return;
+        if (a.n_splits > 1) return;   // (the joining kernel sees to it)
         for (int x = tid; x < n_pairs * D; x += NW * 64) {
             const int pair = tile.first + x / D, row = pair / a.group, hq = hkv * a.group + pair % a.group;
             a.o[(seq.first + row) * a.o_row + hq * a.o_head + x % D] = (__bf16)__builtin_nanf("");
@@ -419,202 +445,326 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
         return;
     }
     // rows of the tile by index of their kind
-    const int sum0 = seq.start - tile.text0, base = tile.text ? tile.text0 : sum0;
-    const int lo = base + ksa_div(tile.first, a.by_group), hi = base + ksa_div(tile.first + n_pairs - 1, a.by_group);
-    const RowKind r_lo = {tile.text, lo}, r_hi = {tile.text, hi};
-    const Visible v_lo = visible(a.rows, r_lo), v_hi = visible(a.rows, r_hi);
+    const int base = tile.text ? tile.text0 : seq.start - tile.text0;
+    auto row_at = [&](int pair) { return RowKind{tile.text, base + ksa_div(tile.first + min(pair, n_pairs - 1), a.by_group)}; };   // (the last one repeats)
+    const Visible v_lo = visible(a.rows, row_at(0)), v_hi = visible(a.rows, row_at(n_pairs - 1));
     const Keys keys = keys_between(v_lo, v_hi);
-    // what every row of the tile sees
-    const Seen every = seen_of(keys, Visible{v_hi.lo_s, v_lo.hi_s, v_hi.lo_t, v_lo.hi_t});
+    // what every row of the tile sees, and every row of the wave
+    auto all_of = [&](const Visible &first, const Visible &last) { return seen_of(keys, Visible{last.lo_s, first.hi_s, last.lo_t, first.hi_t}); };
+    const Seen tile_all = all_of(v_lo, v_hi), wave_all = all_of(visible(a.rows, row_at(wave * 32)), visible(a.rows, row_at(wave * 32 + 31)));
     const int n_tiles = (keys.n + BN - 1) / BN, per = ksa_div(n_tiles + a.n_splits - 1, a.by_splits);
     const int first_tile = split * per, end_tile = min(n_tiles, first_tile + per);
 
-    // the lane's pair
-    const int pair = tile.first + min(wave * 32 + r, n_pairs - 1), in_kind = ksa_div(pair, a.by_group);
-    const RowKind kind = {tile.text, base + in_kind};
-    const int hq = hkv * a.group + pair - in_kind * a.group, row = seq.first + row_of(a.rows, kind) - seq.start;
-    const Seen seen = seen_of(keys, visible(a.rows, kind));
-    const bool w_any = wave * 32 < n_pairs, mine = wave * 32 + r < n_pairs;
+    // packed row and query head of a pair
+    auto place_of = [&](int pair, int &row, int &hq) {
+        const RowKind k = row_at(pair);
+        row = seq.first + row_of(a.rows, k) - seq.start;
+        hq = hkv * a.group + tile.first + min(pair, n_pairs - 1) - (k.idx - base) * a.group;
+    };
+    int q_row, q_head;   // the lane's pair
+    place_of(wave * 32 + r, q_row, q_head);
+    const Seen seen = seen_of(keys, visible(a.rows, row_at(wave * 32 + r)));
     bf16x8 q[KS];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) q[s] = scaled_q(a.q + row * a.q_row + hq * a.q_head + s * 16 + h * 8, a.q_scale);
+    for (int s = 0; s < KS; ++s) q[s] = scaled_q(a.q + q_row * a.q_row + q_head * a.q_head + s * 16 + h * 8, a.q_scale);
 
-    // ---- tiles on their way: where their rows are, then into registers, then as bf16 into LDS -------------------------
-    const unsigned char *kb = a.k + hkv * a.head_bytes, *vb = a.v + hkv * a.head_bytes;
-    const int f_row = lane / LPR, f_piece = lane % LPR;
-    Spot spot;            // of row RW * wave + lane % RW of the tile
-    int ke = 0, ve = 0;
-    u32x4 kr[NI], vr[NI];
-    auto look = [&](int t) { spot = spot_of(a.rows, tile.b, key_at(keys, min(t * BN + RW * wave + lane % RW, keys.n - 1))); };
-    bool lost = false;
-    auto fetch = [&]() {
-        const int64_t off = spot_bytes(a, spot);
-        lost = spot.page < 0;
-        if constexpr (F8) {
-            const int64_t at = spot_exp(a, spot, hkv);
-            ke = a.k_exp[at], ve = a.v_exp[at];
-        }
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const int64_t from = lane_value(off, i * RPI + f_row) + f_piece * 16;
-            kr[i] = *reinterpret_cast<const u32x4 *>(kb + from), vr[i] = *reinterpret_cast<const u32x4 *>(vb + from);
-        }
+    // ---- tiles on their way: table entries two tiles ahead, rows into registers one ahead, then as bf16 into LDS; V a step behind K --
+    const unsigned char *const kb = a.k + hkv * a.head_bytes, *const vb = a.v + hkv * a.head_bytes;
+    const int f_row = lane / LPR % RPI, f_piece = lane % LPR;   // (lanes beyond the rows repeat them)
+    Entry entry;                               // of row RW * wave + lane % RW of a tile
+    int64_t next_at = 0;                       // where that row of the next K tile lies
+    int64_t exp_at = 0;                        // ... and its exponents
+    int k_e = 0, v_e = 0, next_v_e = 0;
+    int64_t from[NI];                          // where the rows of the lane's loads lie: the V tile's, then the K tile's
+    u32x4 rows[NI];                            // ... of V in half 0, of K in half 1
+    bool lost = false, next_lost = false, odd = false;   // row lane % RW of the K tile on its way has no page; elements of V were taken out
+    auto look = [&](int t) { entry = entry_of(a.rows, tile.b, key_at(keys, min(t * BN + RW * wave + lane % RW, keys.n - 1))); };
+    auto settle = [&]() {
+        const Spot spot = spot_of(a.rows, entry);
+        next_lost = spot.page < 0;
+        next_at = spot_bytes(a, spot);
+        if constexpr (F8) exp_at = spot_exp(a, spot, hkv);
     };
-    auto put = [&](int t, int buf) {
-        unsigned char *const to = lds + buf * 2 * BYTES;
-        const bool whole = every.sees_all(t * BN, t * BN + BN);
-        bool odd = false;
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const int at = i * RPI + f_row, y = RW * wave + at;
-            u32x4 k[F8 ? 2 : 1], v[F8 ? 2 : 1];
-            as_bf16<F8>(kr[i], F8 ? power_of_two(__shfl(ke, at)) : 1.f, k);
-            as_bf16<F8>(vr[i], F8 ? power_of_two(__shfl(ve, at)) : 1.f, v);
-#pragma unroll
-            for (int z = 0; z < (F8 ? 2 : 1); ++z) {
-                const int piece = f_piece * (F8 ? 2 : 1) + z;
-                if (!whole) odd |= take_out(v[z]);
-                *reinterpret_cast<u32x4 *>(to + y * (D * 2) + ((piece ^ k_swz<D>(y)) << 4)) = k[z];
-                *reinterpret_cast<u32x4 *>(to + BYTES + y * (D * 2) + ((piece ^ v_swz<D>(y)) << 4)) = v[z];
-            }
+    auto load_v = [&](int i) {
+        if (F8 && i == 0) v_e = next_v_e;
+        rows[i] = *reinterpret_cast<const u32x4 *>(vb + from[i]);
+    };
+    auto find_k = [&](int i) { from[i] = lane_value(next_at, i * RPI + f_row) + f_piece * 16; };
+    auto load_k = [&](int i) {
+        if (i == 0) {
+            lost = next_lost;
+            if constexpr (F8) k_e = a.k_exp[exp_at], next_v_e = a.v_exp[exp_at];
         }
-        const uint64_t none = __builtin_amdgcn_ballot_w64(lost), taken = __builtin_amdgcn_ballot_w64(odd);
-        if (lane == 0) {
-            reinterpret_cast<uint16_t *>(&sh_lost[buf])[wave] = (uint16_t)none;
-            sh_odd[buf][wave] = taken != 0;
-        }
+        rows[i] = *reinterpret_cast<const u32x4 *>(kb + from[i]);
+    };
+    auto put = [&](const u32x4 &x, int e, int i, unsigned char *to) {
+        u32x4 y[F8 ? 2 : 1];
+        as_bf16<F8>(x, F8 ? power_of_two(__shfl(e, i * RPI + f_row)) : 1.f, y);
+#pragma unroll
+        for (int z = 0; z < (F8 ? 2 : 1); ++z) *reinterpret_cast<u32x4 *>(to + z * 16) = y[z];
+    };
+    const int put_k_at = (RW * wave + f_row) * KROW + f_piece * (F8 ? 32 : 16), put_v_at = 2 * K_BYTES + (RW * wave + f_row) * VROW + f_piece * (F8 ? 32 : 16);
+    auto put_k = [&](int t, int i) { put(rows[i], k_e, i, lds + (t & 1) * K_BYTES + put_k_at + i * RPI * KROW); };
+    auto put_v = [&](int t, int i) { put(rows[i], v_e, i, lds + (t & 1) * V_BYTES + put_v_at + i * RPI * VROW); };
+    auto put_state = [&](int t) {   // with K tile t and V tile t - 1
+        const unsigned none = (unsigned)__builtin_amdgcn_ballot_w64(lost) & ((1u << RW) - 1), taken = __builtin_amdgcn_ballot_w64(odd) != 0 ? 1u << 31 : 0u;
+        if (lane == 0) sh_state[t & 1][wave] = none | taken;
     };
 
-    f32x16 o[DB];
+    f32x16 o[DB], sc[2];
+    bf16x8 p[2][2];
+    float m_run = LOWEST, l_run = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int g = 0; g < 16; ++g) o[db][g] = 0.f;
-    float m_run = LOWEST, l_run = 0.f;
+    unsigned any_state = 0, ever = 0;
     const int grp = lane >> 4, li = lane & 15;
-    const int t_row = 4 * (grp >> 1) + (li >> 2), t_col = 16 * (grp & 1) + 4 * (li & 3);
-    const int ll_k = r * (D * 2) + ((k_swz<D>(r) ^ h) << 4);
-    const int ll_v = BYTES + t_row * (D * 2) + (((t_col >> 3) ^ v_swz<D>(t_row)) << 4) + ((t_col & 7) << 1);
+    const int k_at = r * KROW + h * 16, v_at = 2 * K_BYTES + (4 * (grp >> 1) + (li >> 2)) * VROW + 32 * (grp & 1) + 8 * (li & 3);
 
-    if (first_tile < end_tile) {
-        look(first_tile);
-        fetch();
-        look(first_tile + 1);
-        put(first_tile, 0);
-        fetch();
-        look(first_tile + 2);
-    }
-    __syncthreads();
-    for (int t = first_tile; t < end_tile; ++t) {
-        const int buf = (t - first_tile) & 1, x0 = t * BN;
-        const unsigned char *const at = lds + buf * 2 * BYTES;
-        const uint64_t none = sh_lost[buf];
-        if (w_any && __builtin_amdgcn_ballot_w64(seen.sees_any(x0, x0 + BN)) != 0) {
-            f32x16 s[2];
+    // Half y of step t.  SCORES: of keys 32 y .. of K tile t, into sc[y].  WEIGHTS: of sc[y ^ 1] (half 0: tile t - 1, half 1: tile t) into
+    // p[y ^ 1].  OUT: V tile t - 1, keys 32 y .., times p[y].  A slot is one MFMA and what the vector unit does beside it, pinned by fences;
+    // beside(x) is what slot x of the half does for the tiles on their way.
+    constexpr int AHEAD = 3, AHEAD_V = 2;   // operands are read so many slots before the MFMAs that use them
+    bf16x8 k[KS];
+    auto read_k = [&](int t, int y, int x) { k[x] = *reinterpret_cast<const bf16x8 *>(lds + (t & 1) * K_BYTES + y * 32 * KROW + k_at + x * 32); };
+    auto half = [&](int t, auto y_tag, auto scores_tag, auto weights_tag, auto out_tag, auto &&beside) {
+        constexpr int y = decltype(y_tag)::value;
+        constexpr bool SCORES = decltype(scores_tag)::value, WEIGHTS = decltype(weights_tag)::value, OUT = decltype(out_tag)::value;
+        constexpr int EACH = 16 / (2 * KS);   // weights per slot
+        static_assert(2 * DB == KS, "as many slots with V as with K");
+        float ex[16], sum = 0.f;
+        auto weight = [&](int slot) {   // the three steps of a weight lie in slots one after the other
+            if constexpr (WEIGHTS) {
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
-#pragma unroll
-                for (int g = 0; g < 16; ++g) s[y][g] = 0.f;
-#pragma unroll
-            for (int x = 0; x < KS; ++x)
-#pragma unroll
-                for (int y = 0; y < 2; ++y)
-                    s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(at + ((ll_k ^ (x << 5)) + y * 32 * (D * 2))), q[x], s[y], 0, 0, 0);
-            const bool whole = none == 0 && __builtin_amdgcn_ballot_w64(!seen.sees_all(x0, x0 + BN)) == 0;
-            float mx = LOWEST;
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-#pragma unroll
-                for (int g = 0; g < 16; ++g) s[y][g] *= a.score_scale;
-            if (!whole) {
-#pragma unroll
-                for (int y = 0; y < 2; ++y)
-#pragma unroll
-                    for (int g = 0; g < 16; ++g) {
-                        const int key = y * 32 + 8 * (g / 4) + 4 * h + g % 4;
-                        s[y][g] = !seen.sees(x0 + key) ? -INFINITY : (none >> key) & 1 ? __builtin_nanf("") : s[y][g];
+                for (int i = 0; i < EACH; ++i) {
+                    const int g = (slot - 2) * EACH + i;
+                    if (g >= 0 && g < 16) {
+                        sum += ex[g];
+                        if (g & 1) p[y ^ 1][g / 8][g % 8 - 1] = (__bf16)ex[g - 1], p[y ^ 1][g / 8][g % 8] = (__bf16)ex[g];
+                        if (g % 8 == 7) asm volatile("" : "+v"(p[y ^ 1][g / 8]), "+v"(sum));   // (in this slot and not where it is used)
                     }
+                }
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) {
+                    const int g = (slot - 1) * EACH + i;
+                    if (g >= 0 && g < 16) {
+                        ex[g] = __builtin_amdgcn_exp2f(ex[g]);
+                        asm volatile("" : "+v"(ex[g]));
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) {
+                    const int g = slot * EACH + i;
+                    if (g < 16) {
+                        ex[g] = fmaf(sc[y ^ 1][g], a.score_scale, -m_run);
+                        asm volatile("" : "+v"(ex[g]));
+                    }
+                }
             }
+        };
+        bf16x8 v[2 * DB];
+        const unsigned char *const from_v = lds + ((t - 1) & 1) * V_BYTES + y * 32 * VROW + v_at;
+        auto read_v = [&](int x) {   // 16 keys x / DB, columns 32 (x % DB) ..
+            if constexpr (OUT) {
+                const unsigned char *at = from_v + x / DB * 16 * VROW + x % DB * 64;
+                const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(at));
+                const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(at + 8 * VROW));
+                v[x] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        };
+        if constexpr (SCORES && y == 0) {   // (those of half 1 have been read in half 0)
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
+            for (int x = 0; x < AHEAD; ++x) read_k(t, 0, x);
+        }
+        KSA_FENCE();
 #pragma unroll
-                for (int g = 0; g < 16; ++g) mx = fmaxf(mx, s[y][g]);
-            if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
-                mx = fmaxf(fmaxf(mx, swap32(mx)), m_run);
-                const float alpha = __builtin_amdgcn_exp2f(m_run - mx);
-                m_run = mx, l_run *= alpha;
+        for (int x = 0; x < KS; ++x) {
+            if (x + AHEAD < KS) {
+                if constexpr (SCORES) read_k(t, y, x + AHEAD);
+            } else if (x + AHEAD < KS + AHEAD_V) {
+                read_v(x + AHEAD - KS);
+            }
+            if constexpr (SCORES) {
+                if (x == 0) {
+#pragma unroll
+                    for (int g = 0; g < 16; ++g) sc[y][g] = 0.f;
+                }
+                sc[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[x], q[x], sc[y], 0, 0, 0);
+            }
+            weight(x);
+            beside(x);
+            KSA_FENCE();
+        }
+#pragma unroll
+        for (int x = 0; x < KS; ++x) {
+            if (x + AHEAD_V < KS) read_v(x + AHEAD_V);
+            else if (SCORES && y == 0) read_k(t, 1, x + AHEAD_V - KS);
+            if constexpr (OUT) o[x % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[x], p[y][x / DB], o[x % DB], 0, 0, 0);
+            weight(KS + x);
+            beside(KS + x);
+            KSA_FENCE();
+        }
+        if constexpr (SCORES && y == 0) {
+#pragma unroll
+            for (int x = AHEAD_V; x < AHEAD; ++x) read_k(t, 1, x);
+        }
+        weight(2 * KS), weight(2 * KS + 1);
+        if constexpr (WEIGHTS) {
+            if (__builtin_amdgcn_ballot_w64(sum > HIGH) != 0) {
+                float most = sc[y ^ 1][0];
+#pragma unroll
+                for (int g = 1; g < 16; ++g) most = fmaxf(most, sc[y ^ 1][g]);
+                most = fmaxf(most, swap32(most)) * a.score_scale;
+                const float m = fmaxf(sum, swap32(sum)) > HIGH ? fmaxf(most, m_run) : m_run;   // (by the row alone)
+                const float alpha = __builtin_amdgcn_exp2f(m_run - m);
+                m_run = m, l_run *= alpha, sum = 0.f;
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
 #pragma unroll
                     for (int g = 0; g < 16; ++g) o[db][g] *= alpha;
-            }
-            bf16x8 p[4];
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
 #pragma unroll
                 for (int g = 0; g < 16; ++g) {
-                    const float w = __builtin_amdgcn_exp2f(s[y][g] - m_run);
-                    l_run += w;
-                    p[2 * y + g / 8][g % 8] = (__bf16)w;
+                    const float w = __builtin_amdgcn_exp2f(fmaf(sc[y ^ 1][g], a.score_scale, -m_run));
+                    sum += w, p[y ^ 1][g / 8][g % 8] = (__bf16)w;
                 }
+            }
+            l_run += sum;
+        }
+        if constexpr (SCORES) {
+            const int x0 = t * BN + 32 * y;
+            if (!wave_all.sees_all(x0, x0 + 32) || any_state != 0) {
+                unsigned none = 0;   // keys without a page
 #pragma unroll
-            for (int y = 0; y < 4; ++y)
+                for (int x = 0; x < NW / 2; ++x) none |= (sh_state[t & 1][y * (NW / 2) + x] & ((1u << RW) - 1)) << (x * RW);
 #pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    const unsigned char *from = at + y * 16 * (D * 2) + (ll_v ^ (db << 6));
-                    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(from));
-                    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(from + 8 * (D * 2)));
-                    const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[y], o[db], 0, 0, 0);
-                }
-            if ((sh_odd[buf][0] | sh_odd[buf][1] | sh_odd[buf][2] | sh_odd[buf][3]) != 0) {
-                for (int key = 0; key < BN; ++key) {
-                    const Spot sp = spot_of(a.rows, tile.b, key_at(keys, min(x0 + key, keys.n - 1)));
-                    const bool see = seen.sees(x0 + key);
-#pragma unroll
-                    for (int db = 0; db < DB; ++db)
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            float y[4];
-                            no_numbers<F8>(a, hkv, sp, db * 32 + 8 * g + 4 * h, y);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[db][4 * g + e] += see ? y[e] : 0.f;
-                        }
+                for (int g = 0; g < 16; ++g) {
+                    const int key = 8 * (g / 4) + 4 * h + g % 4;
+                    const float lost_or_not = (none >> key) & 1 ? __builtin_nanf("") : sc[y][g];
+                    sc[y][g] = seen.sees(x0 + key) ? lost_or_not : -INFINITY;
                 }
             }
         }
-        if (t + 1 < end_tile) {
-            put(t + 1, buf ^ 1);
-            fetch();
-            look(t + 3);
-        }
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    const std::integral_constant<int, 0> y0;
+    const std::integral_constant<int, 1> y1;
+    // Slots of a half: KS, and as many again.  Half 0 brings V of this tile to LDS, half 1 K of the next; where the rows of the one after that
+    // are, is worked out on the way.
+    auto bring_v = [&](int t) {
+        return [&, t](int x) {
+            if (x < NI) load_v(x);
+            if (x >= NI && x < 2 * NI) find_k(x - NI);
+            if (x == 2 * KS - NI) {
+                odd = false;
+                if (!tile_all.sees_all(t * BN, t * BN + BN)) {
+#pragma unroll
+                    for (int i = 0; i < NI; ++i) odd |= take_out_raw<F8>(rows[i]);
+                }
+            }
+            if (x >= 2 * KS - NI) put_v(t, x - (2 * KS - NI));
+        };
+    };
+    auto bring_k = [&](int t) {
+        return [&, t](int x) {
+            if (x < NI) load_k(x);
+            if (x == NI) settle();
+            if (x == NI + 1) look(t + 2);
+            if (x == 2 * KS - NI) put_state(t);
+            if (x >= 2 * KS - NI) put_k(t, x - (2 * KS - NI));
+        };
+    };
+    static_assert(3 * NI <= 2 * KS, "in one half");
+    auto nothing = [](int) {};
+    auto begin = [&](int t) {
         __syncthreads();
+        unsigned state = 0;
+#pragma unroll
+        for (int x = 0; x < NW; x += 4) {
+            const u32x4 four = *reinterpret_cast<const u32x4 *>(sh_state[t & 1] + x);
+            state |= four[0] | four[1] | four[2] | four[3];
+        }
+        any_state = __builtin_amdgcn_readfirstlane(state);
+        ever |= any_state;
+    };
+
+    if (first_tile < end_tile) {
+        look(first_tile);
+        settle();
+#pragma unroll
+        for (int i = 0; i < NI; ++i) find_k(i), load_k(i);
+        look(first_tile + 1);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) put_k(first_tile, i);
+        put_state(first_tile);
+        settle();
+        look(first_tile + 2);
+        begin(first_tile);
+        half(first_tile, y0, Yes{}, No{}, No{}, bring_v(first_tile));
+        half(first_tile, y1, Yes{}, Yes{}, No{}, bring_k(first_tile + 1));
+        for (int t = first_tile + 1; t < end_tile; ++t) {
+            begin(t);
+            half(t, y0, Yes{}, Yes{}, Yes{}, bring_v(t));
+            half(t, y1, Yes{}, Yes{}, Yes{}, bring_k(t + 1));
+        }
+        begin(end_tile);
+        half(end_tile, y0, No{}, Yes{}, Yes{}, nothing);
+        half(end_tile, y1, No{}, No{}, Yes{}, nothing);
     }
 
     // ---- results ---------------------------------------------------------------------------------------------------------
+    if (ever >> 31) {   // what was taken out of V, to the rows that see it
+#pragma unroll 1
+        for (int x = first_tile * BN; x < min(end_tile * BN, keys.n); ++x) {
+            if (tile_all.sees_all(x / BN * BN, x / BN * BN + BN)) continue;
+            const Spot sp = spot_of(a.rows, entry_of(a.rows, tile.b, key_at(keys, x)));
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    float z[4];
+                    no_numbers<F8>(a, hkv, sp, db * 32 + 8 * g + 4 * h, z);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[db][4 * g + e] += seen.sees(x) ? z[e] : 0.f;
+                }
+        }
+    }
     const float l = l_run + swap32(l_run);
-    if (!mine) return;
-    if (a.n_splits == 1) {
-        __bf16 *to = a.o + row * a.o_row + hq * a.o_head;
-        const float inv = 1.f / l;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                bf16x4 y;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[db][4 * g + e] * inv);
-                *reinterpret_cast<bf16x4 *>(to + db * 32 + 8 * g + 4 * h) = y;
-            }
-        if (a.lse && h == 0) a.lse[(int64_t)row * a.n_q_heads + hq] = log_sum(m_run, l);
-    } else {
-        float *rec = a.ws + (((int64_t)row * a.n_q_heads + hq) * a.n_splits + split) * (D + 4);
+    const bool mine = wave * 32 + r < n_pairs;
+    if (a.n_splits > 1) {
+        if (!mine) return;
+        float *rec = a.ws + (((int64_t)q_row * a.n_q_heads + q_head) * a.n_splits + split) * (D + 4);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<f32x4 *>(rec + db * 32 + 8 * g + 4 * h) = f32x4{o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]};
         if (h == 0) rec[D] = m_run, rec[D + 1] = l;
+        return;
+    }
+    if (a.lse && h == 0 && mine) a.lse[(int64_t)q_row * a.n_q_heads + q_head] = log_sum(m_run, l);
+    // whole rows are stored: through memory of the wave's own, where the tiles were
+    __syncthreads();
+    unsigned char *const stage = lds + wave * 32 * STAGE_ROW;
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            bf16x4 z;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] = (__bf16)(o[db][4 * g + e] * inv);
+            *reinterpret_cast<bf16x4 *>(stage + r * STAGE_ROW + (db * 32 + 8 * g + 4 * h) * 2) = z;
+        }
+    constexpr int OUT_LANES = D / 8, OUT_ROWS = 64 / OUT_LANES;
+#pragma unroll
+    for (int i = 0; i < 32 / OUT_ROWS; ++i) {
+        const int at = i * OUT_ROWS + lane / OUT_LANES;
+        const u32x4 z = *reinterpret_cast<const u32x4 *>(stage + at * STAGE_ROW + lane % OUT_LANES * 16);
+        int to_row, to_head;
+        place_of(wave * 32 + at, to_row, to_head);
+        if (wave * 32 + at < n_pairs) *reinterpret_cast<u32x4 *>(a.o + to_row * a.o_row + to_head * a.o_head + lane % OUT_LANES * 8) = z;
     }
 }
 
@@ -662,7 +812,11 @@ void launch(const FwdArgs &a, const KsaPagedPlan &plan, hipStream_t st) {
     const dim3 few(plan.n_splits, a.n_kv_heads, a.rows.batch);
     if (plan.columns == 16) hipLaunchKernelGGL((ksa_paged_few_kernel<D, F8, 16>), few, dim3(FEW_WAVES * 64), 0, st, a);
     else if (plan.columns == 32) hipLaunchKernelGGL((ksa_paged_few_kernel<D, F8, 32>), few, dim3(FEW_WAVES * 64), 0, st, a);
-    else hipLaunchKernelGGL((ksa_paged_many_kernel<D, F8>), dim3((unsigned)(plan.slots * plan.n_splits * a.n_kv_heads)), dim3(NW * 64), 0, st, a);
+    else {
+        const dim3 many((unsigned)(plan.slots * plan.n_splits * a.n_kv_heads));
+        if (plan.pairs == 128) hipLaunchKernelGGL((ksa_paged_many_kernel<D, F8, 4>), many, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((ksa_paged_many_kernel<D, F8, 8>), many, dim3(512), 0, st, a);
+    }
     if (plan.n_splits > 1)
         hipLaunchKernelGGL((ksa_paged_join_kernel<D>), dim3((unsigned)(((int64_t)a.rows.total * a.n_q_heads + 3) / 4)), dim3(256), 0, st, a);
 }

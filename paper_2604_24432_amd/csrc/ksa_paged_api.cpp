@@ -67,16 +67,19 @@ int64_t most_keys(const ksa_params *p, int64_t max_rows) {
 
 KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_rows, int32_t n_splits) {
     const int32_t group = p->n_q_heads / p->n_kv_heads;
-    KsaPagedPlan plan = {0, 1, 0};
+    KsaPagedPlan plan = {0, 1, 0, 0};
     const int64_t pairs = max_rows * group, keys = most_keys(p, max_rows);
     int64_t units, want, least;   // workgroups of one span; how many are wanted; keys of a span
     if (pairs <= 32) {
         plan.columns = pairs <= 16 ? 16 : 32;
         units = (int64_t)p->batch * p->n_kv_heads, want = 1024, least = 256;
     } else {
-        // every sequence ends one tile of text and one of summaries before it is full
-        plan.slots = (int32_t)((total_rows * group) / KSA_PAGED_PAIRS + (p->n_summary > 0 ? 2 : 1) * (int64_t)p->batch);
-        units = (int64_t)plan.slots * p->n_kv_heads, want = 512, least = 512;
+        // Tiles of 256 pairs take their keys from memory half as often, but fill a compute unit alone: where there are as many as units
+        // (full attention, 2048 rows, 64K keys, 32/8 heads: 128 pairs 2194 us, 256 2020; 8-bit, 4608 rows, 128K 1095, 1017; window of 1023, 1280
+        // rows, 16/16 heads 43, 56).  Every sequence ends one tile of text and one of summaries before it is full.
+        plan.pairs = total_rows * p->n_q_heads >= 256 * 256 ? 256 : 128;
+        plan.slots = (int32_t)((total_rows * group) / plan.pairs + (p->n_summary > 0 ? 2 : 1) * (int64_t)p->batch);
+        units = (int64_t)plan.slots * p->n_kv_heads, want = plan.pairs == 256 ? 256 : 512, least = 512;
     }
     plan.n_splits = n_splits;
     if (n_splits == 0) plan.n_splits = (int32_t)std::max<int64_t>(1, std::min({want / units, keys / least, (int64_t)64}));

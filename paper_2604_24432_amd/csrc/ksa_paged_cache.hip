@@ -35,7 +35,7 @@ __device__ __forceinline__ Place place_of(const MoveArgs &a) {
     const NewRows r = new_rows(a.rows, b, a.rows.total);
     p.any = p.row >= r.first && p.row < r.first + r.n;
     if (!p.any || !r.ok) return p;
-    const Spot s = spot_of(a.rows, b, kind_of(a.rows, r.start + (p.row - r.first)));
+    const Spot s = spot_of(a.rows, entry_of(a.rows, b, kind_of(a.rows, r.start + (p.row - r.first))));
     p.page = s.page, p.slot = s.slot;
     return p;
 }

@@ -50,19 +50,23 @@ KSA_INDEX int text_before(const PagedRows &a, int row) {   // text rows among th
     return j * a.c + min(row - j * (a.c + a.m), a.c);
 }
 
-// Where a row of one of the tables lies.  page < 0: nowhere.
+// Where a row of one of the tables lies, in two steps, so that the first one's load may be on its way for a while.  entry_of: what the table
+// says (its last column stands in for one behind it).  spot_of: page < 0 for no page.
+struct Entry {
+    int page, slot;
+    bool inside;
+};
 struct Spot {
     int page, slot;
 };
-KSA_INDEX Spot spot_of(const PagedRows &a, int b, RowKind k) {
-    const int col = k.idx >> a.shift, cols = k.text ? a.text_cols : a.sum_cols;
-    Spot s = {-1, k.idx & ((1 << a.shift) - 1)};
-    if (col < cols) {
-        const int page = (k.text ? a.text_table : a.sum_table)[(int64_t)b * cols + col];
-        s.page = (unsigned)page < (unsigned)a.n_pages ? page : -1;
-    }
-    return s;
+KSA_INDEX Entry entry_of(const PagedRows &a, int b, RowKind k) {
+    // (values first: a choice between members of `a` is one between their addresses, and so a load from memory)
+    const int32_t *const of_text = a.text_table, *const of_sums = a.sum_table, *const table = k.text ? of_text : of_sums;
+    const int text_cols = a.text_cols, sum_cols = a.sum_cols, cols = k.text ? text_cols : sum_cols;
+    const int col = k.idx >> a.shift;
+    return {table[(int64_t)b * cols + min(col, cols - 1)], k.idx & ((1 << a.shift) - 1), col < cols};
 }
+KSA_INDEX Spot spot_of(const PagedRows &a, const Entry &e) { return {(e.inside & ((unsigned)e.page < (unsigned)a.n_pages)) ? e.page : -1, e.slot}; }
 
 // What a row sees (Eq. 3): summaries [lo_s, hi_s), text [lo_t, hi_t).
 struct Visible {
@@ -108,9 +112,10 @@ KSA_INDEX Keys keys_of(const PagedRows &a, int from, int to) {
 // A row's keys as positions of the list: [a, b) and [c, d), joined to one where they meet.
 struct Seen {
     int a, b, c, d;
-    KSA_INDEX bool sees(int x) const { return (x >= a && x < b) || (x >= c && x < d); }
-    KSA_INDEX bool sees_all(int x, int end) const { return (x >= a && end <= b) || (x >= c && end <= d); }
-    KSA_INDEX bool sees_any(int x, int end) const { return max(x, a) < min(end, b) || max(x, c) < min(end, d); }
+    // (no && and ||: they would become branches)
+    KSA_INDEX bool sees(int x) const { return ((x >= a) & (x < b)) | ((x >= c) & (x < d)); }
+    KSA_INDEX bool sees_all(int x, int end) const { return ((x >= a) & (end <= b)) | ((x >= c) & (end <= d)); }
+    KSA_INDEX bool sees_any(int x, int end) const { return (max(x, a) < min(end, b)) | (max(x, c) < min(end, d)); }
 };
 KSA_INDEX Seen seen_of(const Keys &k, const Visible &v) {
     Seen s = {v.lo_s - k.s0, v.hi_s - k.s0, v.lo_t - k.t0 + k.n_s, v.hi_t - k.t0 + k.n_s};

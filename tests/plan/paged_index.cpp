@@ -103,7 +103,7 @@ int main() {
     for (int b = 0; b < 2; ++b)
         for (int idx : {0, 7, 8, 15, 16, 23, 24, 31, 1000, INT32_MAX})
             for (int kind = 0; kind < 2; ++kind) {
-                const Spot s = spot_of(a, b, RowKind{kind == 1, idx});
+                const Spot s = spot_of(a, entry_of(a, b, RowKind{kind == 1, idx}));
                 const int col = idx / 8, cols = kind ? 3 : 1, entry = col < cols ? (kind ? text[b][col] : sums[b][col]) : -1;
                 const int want = entry >= 0 && entry < 5 ? entry : -1;
                 if (s.page != want || s.slot != idx % 8) fail("page", b, idx);

@@ -88,6 +88,8 @@ MANY = [
     (6, 2, 64, 8, 8, 0, 16, [203, 8], [160, 90]),
     (1, 1, 64, 128, 16, 1, 1024, [0], [1000]),
     (200, 1, 64, 8, 1, 2, 8, [30], [3]),                                         # more heads than a tile has pairs
+    (32, 2, 128, 64, 8, 1, 16, [333, 0, 71], [1100, 900, 201]),                  # 65536 pairs and more: larger tiles
+    (64, 64, 64, 48, 6, 2, 64, [10, 700], [900, 311]),
 ]
 
 
