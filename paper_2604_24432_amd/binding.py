@@ -574,9 +574,23 @@ class PagedCache:
         self.struct = ksa_paged_cache(KSA_CACHE_FP8 if f8 else KSA_CACHE_BF16, rows, n_pages, text_table.shape[1],
                                       summary_table.shape[1] if summary_table is not None else 0, 0, *ptr, _strides_of(k))
 
+        # what a call needs of all this, as it needs it
+        self._args = (C.byref(params), C.byref(self.struct))
+        self._dev, self._batch = k.device.index, ((params.batch + 1,), (params.batch,))
+        self._kv, self._q = (params.n_kv_heads, params.head_dim), (params.n_q_heads, params.head_dim)
+
     @property
     def page_rows(self) -> int:
         return self.struct.page_rows
+
+    def _plain(self, x, y, row, cu_rows, start) -> bool:
+        """Whether x and y are contiguous [rows, *row] tensors and the batch is as it should be, on the cache's device: in as few steps as possible."""
+        import torch
+        dev, shape = self._dev, x.shape
+        return (x.dtype is torch.bfloat16 and y.dtype is torch.bfloat16 and cu_rows.dtype is torch.int32 and start.dtype is torch.int32 and
+                shape == y.shape and shape[1:] == row and (cu_rows.shape, start.shape) == self._batch and x.is_contiguous() and y.is_contiguous() and
+                cu_rows.is_contiguous() and start.is_contiguous() and
+                x.get_device() == dev and y.get_device() == dev and cu_rows.get_device() == dev and start.get_device() == dev)
 
 
 def _strides_of(t):
@@ -611,6 +625,8 @@ def _rows_of_call(cache: PagedCache, tensors, heads, cu_rows, start):
         _require(t, name, torch.int32, 1)
         if t.shape[0] != n:
             raise ValueError(f"{name} must have {n} elements")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
     if any(t.device != cache.device for t, _ in tensors) or cu_rows.device != cache.device or start.device != cache.device:
         raise ValueError("tensors lie on another device than the cache")
 
@@ -618,16 +634,20 @@ def _rows_of_call(cache: PagedCache, tensors, heads, cu_rows, start):
 def _paged(cache: PagedCache, name, stream, *args):
     """The call, on the cache's device: on `stream`, or on that device's current one."""
     from torch import _C
-    if stream is not None and stream.device != cache.device:
+    here, there = _C._cuda_getDevice(), cache._dev
+    if stream is None:
+        raw = _C._cuda_getCurrentRawStream(there)
+    elif stream.device != cache.device:
         raise ValueError("stream belongs to another device than the cache")
-    here, there = _C._cuda_getDevice(), cache.device.index
-    raw = stream.cuda_stream if stream is not None else _C._cuda_getCurrentRawStream(there)
-    if here != there:
+    else:
+        raw = stream.cuda_stream
+    if here == there:
+        rc = getattr(lib(), name)(*cache._args, *args, raw)
+    else:
         _C._cuda_setDevice(there)
-    try:
-        rc = getattr(lib(), name)(C.byref(cache.params), C.byref(cache.struct), *args, raw)
-    finally:
-        if here != there:
+        try:
+            rc = getattr(lib(), name)(*cache._args, *args, raw)
+        finally:
             _C._cuda_setDevice(here)
     if rc:
         _check(rc, name)
@@ -636,23 +656,31 @@ def _paged(cache: PagedCache, name, stream, *args):
 def ksa_paged_append(cache: PagedCache, k_new, v_new, cu_rows, start, stream=None):
     """k_new, v_new [rows, Hkv, d] bf16: rows [cu_rows[b], cu_rows[b + 1]) become sequence b's augmented rows from start[b] on.
     cu_rows int32 [batch + 1] and start int32 [batch] lie on the GPU."""
-    _rows_of_call(cache, ((k_new, "k_new"), (v_new, "v_new")), cache.params.n_kv_heads, cu_rows, start)
-    if not _same_strides(k_new, v_new):
-        raise ValueError("k_new and v_new must have the same strides")
-    _paged(cache, "ksa_paged_append", stream, k_new.data_ptr(), v_new.data_ptr(), _strides_of(k_new), cu_rows.data_ptr(), start.data_ptr(),
-           k_new.shape[0])
+    strides = None
+    if not cache._plain(k_new, v_new, cache._kv, cu_rows, start):
+        _rows_of_call(cache, ((k_new, "k_new"), (v_new, "v_new")), cache.params.n_kv_heads, cu_rows, start)
+        if not _same_strides(k_new, v_new):
+            raise ValueError("k_new and v_new must have the same strides")
+        strides = _strides_of(k_new)
+    _paged(cache, "ksa_paged_append", stream, k_new.data_ptr(), v_new.data_ptr(), strides, cu_rows.data_ptr(), start.data_ptr(), k_new.shape[0])
 
 
 def ksa_paged_read(cache: PagedCache, cu_rows, start, total_rows: int, k=None, v=None, stream=None):
     """The rows that ksa_paged_append with these cu_rows and start would write -> k, v [total_rows, Hkv, d] bf16."""
     import torch
-    shape = (total_rows, cache.params.n_kv_heads, cache.params.head_dim)
-    k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if k is None else k
-    v = torch.empty_like(k) if v is None else v
-    _rows_of_call(cache, ((k, "k"), (v, "v")), shape[1], cu_rows, start)
-    if k.shape[0] != total_rows or not _same_strides(k, v):
-        raise ValueError(f"k and v must be {shape}, with the same strides")
-    _paged(cache, "ksa_paged_read", stream, k.data_ptr(), v.data_ptr(), _strides_of(k), cu_rows.data_ptr(), start.data_ptr(), total_rows)
+    if k is None:
+        k = torch.empty((total_rows, *cache._kv), dtype=torch.bfloat16, device=cache.device)
+    if v is None:
+        v = torch.empty_like(k)
+    strides = None
+    if not cache._plain(k, v, cache._kv, cu_rows, start):
+        _rows_of_call(cache, ((k, "k"), (v, "v")), cache.params.n_kv_heads, cu_rows, start)
+        if not _same_strides(k, v):
+            raise ValueError("k and v must have the same strides")
+        strides = _strides_of(k)
+    if k.shape[0] != total_rows:
+        raise ValueError(f"k and v must have {total_rows} rows")
+    _paged(cache, "ksa_paged_read", stream, k.data_ptr(), v.data_ptr(), strides, cu_rows.data_ptr(), start.data_ptr(), total_rows)
     return k, v
 
 
@@ -662,22 +690,27 @@ def ksa_paged_fwd(cache: PagedCache, q, cu_rows, start, max_rows: Optional[int] 
     max_rows: the largest number of rows of a sequence (all of them if omitted); workspace: uint8, at least
     paged_workspace_bytes(cache, rows, max_rows, n_splits) bytes (allocated here if omitted)."""
     import torch
-    rows, heads = q.shape[0], cache.params.n_q_heads
-    max_rows = max(rows, 1) if max_rows is None else max_rows
+    rows = q.shape[0]
+    if max_rows is None:
+        max_rows = max(rows, 1)
     if o is None:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _rows_of_call(cache, ((q, "q"), (o, "o")), heads, cu_rows, start)
-    if lse is None and return_lse:
-        lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device)
-    if lse is not None:
+        o = torch.empty_like(q)
+    q_strides = o_strides = None
+    if not cache._plain(q, o, cache._q, cu_rows, start):
+        _rows_of_call(cache, ((q, "q"), (o, "o")), cache.params.n_q_heads, cu_rows, start)
+        q_strides, o_strides = _strides_of(q), _strides_of(o)
+    if lse is None:
+        if return_lse:
+            lse = q.new_empty((rows, cache.params.n_q_heads), dtype=torch.float32)
+    else:
         _require(lse, "lse", torch.float32, 2)
-        if tuple(lse.shape) != (rows, heads) or not lse.is_contiguous() or lse.device != cache.device:
-            raise ValueError(f"lse must be contiguous {(rows, heads)} on the cache's device")
+        if tuple(lse.shape) != (rows, cache.params.n_q_heads) or not lse.is_contiguous() or lse.device != cache.device:
+            raise ValueError(f"lse must be contiguous {(rows, cache.params.n_q_heads)} on the cache's device")
     if workspace is None:
-        workspace = torch.empty(paged_workspace_bytes(cache, rows, max_rows, n_splits), dtype=torch.uint8, device=q.device)
-    if workspace.device != cache.device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        workspace = torch.empty(paged_workspace_bytes(cache, rows, max_rows, n_splits), dtype=torch.uint8, device=cache.device)
+    elif workspace.dtype is not torch.uint8 or workspace.get_device() != cache._dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
-    _paged(cache, "ksa_paged_fwd", stream, q.data_ptr(), o.data_ptr(), lse.data_ptr() if lse is not None else None, _strides_of(q), _strides_of(o),
+    _paged(cache, "ksa_paged_fwd", stream, q.data_ptr(), o.data_ptr(), lse.data_ptr() if lse is not None else None, q_strides, o_strides,
            cu_rows.data_ptr(), start.data_ptr(), rows, max_rows, workspace.data_ptr(), workspace.numel(), n_splits)
     return o, lse
 

@@ -24,9 +24,10 @@ struct KsaPagedMove {
 int ksa_launch_paged_append(const KsaPagedMove &a, void *stream);
 int ksa_launch_paged_read(const KsaPagedMove &a, void *stream);
 
+#define KSA_PAGED_FEW 32
 // How the attention of a call is dealt to workgroups.
 struct KsaPagedPlan {
-    int32_t columns;              // 16 or 32: the kernel for few rows, with so many (row, query head) pairs at most; 0: the one for many
+    bool few;                     // the kernel for few rows: at most KSA_PAGED_FEW (row, query head) pairs of a sequence and KV head
     int32_t n_splits;             // spans of the keys
     int32_t pairs;                // many rows: (row, query head) pairs of a query tile, 128 or 256
     int32_t slots;                // ... and query tiles of all sequences, none less

@@ -30,18 +30,13 @@ struct FwdArgs {
     int64_t q_row, q_head, o_row, o_head;
     int32_t max_rows;
     int32_t n_q_heads, n_kv_heads, group, n_splits;
-    KsaDivisor by_group, by_heads, by_splits;
+    KsaDivisor by_group, by_heads, by_splits, by_q_heads;
     float q_scale, score_scale;   // scale * log2(e) in two factors, the first a power of two that goes into q
 };
 
 constexpr float LOWEST = -FLT_MAX;
 
-// values of lane l ^ 16 and l ^ 32
-__device__ __forceinline__ float swap16(float x) {
-    const unsigned u = __builtin_bit_cast(unsigned, x);
-    auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    return __builtin_bit_cast(float, (threadIdx.x & 16) ? r[0] : r[1]);
-}
+// value of lane l ^ 32
 __device__ __forceinline__ float swap32(float x) {
     const unsigned u = __builtin_bit_cast(unsigned, x);
     auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
@@ -88,6 +83,19 @@ __device__ __forceinline__ bool take_out(u32x4 &x) {
     }
     return any;
 }
+// Bytes of an 8-bit word (halves of a word of bf16) that are no numbers become zero; whether there were any.
+template <bool F8>
+__device__ __forceinline__ bool take_out_raw(u32x4 &x) {
+    if constexpr (!F8) return take_out(x);
+    unsigned any = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const unsigned hit = ((x[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // (0x7f and 0xff are the NaNs)
+        any |= hit, x[e] &= ~((hit >> 7) * 0xffu);
+    }
+    return any != 0;
+}
+
 // four elements of a V row from column d on; those that are numbers are zero
 template <bool F8>
 __device__ __forceinline__ void no_numbers(const FwdArgs &a, int hkv, const Spot &s, int d, float (&y)[4]) {
@@ -112,239 +120,9 @@ __device__ __forceinline__ bf16x8 scaled_q(const __bf16 *q, float by) {
 
 __device__ __forceinline__ float log_sum(float m, float l) { return (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f; }
 
-// ---- few rows -----------------------------------------------------------------------------------------------------------
-
-constexpr int FEW_WAVES = 4, BLOCK = 32;   // keys of a wave's step
-
-// The 16-byte pieces of a V row in LDS are dealt by this function of the row: the 8 rows that two groups of 16 lanes read 32 bytes of each
-// (transposing reads) lie in different banks.
-template <int D>
-__device__ __forceinline__ int few_swz(int row) { return (D == 128 ? (row & 3) << 2 : (row & 2) << 1) ^ ((row & 4) >> 1); }
-
-template <int D, bool F8, int NC>
-__global__ __launch_bounds__(FEW_WAVES * 64) void ksa_paged_few_kernel(const FwdArgs a) {
-    constexpr int CB = NC / 16, KS = D / 32, DB = D / 16, ES = F8 ? 1 : 2;
-    constexpr int KL = D * ES / 64;          // loads per 16 keys of K: 64 bytes of each
-    constexpr int LPR = D * ES / 16;         // lanes per V row
-    constexpr int RPW = 64 / LPR, VL = BLOCK / RPW;
-    constexpr int OUT_ROW = D + 4;
-    __shared__ __align__(16) unsigned char lds[FEW_WAVES * 16 * OUT_ROW * 4];
-    __shared__ float sh_m[FEW_WAVES][NC], sh_l[FEW_WAVES][NC];
-    static_assert(FEW_WAVES * 16 * OUT_ROW * 4 >= FEW_WAVES * BLOCK * D * 2, "the results lie where the V blocks were");
-
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col = lane & 15, grp = lane >> 4;
-    const int split = blockIdx.x, hkv = blockIdx.y, b = blockIdx.z;
-    const NewRows seq = new_rows(a.rows, b, a.max_rows);
-    if (seq.n == 0) return;
-    if (!seq.ok) {
-        if (a.n_splits > 1) return;   // (the joining kernel sees to it)
-        for (int x = tid; x < seq.n * a.group * D; x += FEW_WAVES * 64) {
-            const int row = x / (a.group * D), h = hkv * a.group + x / D % a.group;
-            a.o[(seq.first + row) * a.o_row + h * a.o_head + x % D] = (__bf16)__builtin_nanf("");
-            if (a.lse && x % D == 0) a.lse[(int64_t)(seq.first + row) * a.n_q_heads + h] = __builtin_nanf("");
-        }
-        return;
-    }
-    const Keys keys = keys_of(a.rows, seq.start, seq.start + seq.n - 1);
-    const int blocks = (keys.n + BLOCK - 1) / BLOCK, per = ksa_div(blocks + a.n_splits - 1, a.by_splits) * BLOCK;
-    const int v0 = split * per, v1 = min(keys.n, v0 + per);
-
-    // pair p = row * group + head, of which column p % 16 of block p / 16 is this lane's (the last one repeats)
-    const int pairs = seq.n * a.group;
-    bf16x8 q[CB][KS];
-    Seen seen[CB];
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        const int p = min(cb * 16 + col, pairs - 1), row = ksa_div(p, a.by_group), h = hkv * a.group + p - row * a.group;
-        const __bf16 *from = a.q + (seq.first + row) * a.q_row + h * a.q_head;
-#pragma unroll
-        for (int s = 0; s < KS; ++s)   // (the columns of a step's operand are those that the lane has of a K row)
-            q[cb][s] = scaled_q(from + (F8 ? (s / 2) * 64 + grp * 16 + (s & 1) * 8 : s * 32 + grp * 8), a.q_scale);
-        seen[cb] = seen_of(keys, visible(a.rows, kind_of(a.rows, seq.start + row)));
-    }
-    f32x4 o[CB][DB];
-    float m_run[CB], l_run[CB];
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        m_run[cb] = LOWEST, l_run[cb] = 0.f;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[cb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-
-    unsigned char *const vt = lds + wave * BLOCK * D * 2;
-    const unsigned char *kb = a.k + hkv * a.head_bytes, *vb = a.v + hkv * a.head_bytes;
-    const int t_row = 4 * grp + (col >> 2);
-    const int t_at = t_row * (D * 2) + ((((col & 3) >> 1) ^ few_swz<D>(t_row)) << 4) + ((col & 1) << 3);
-
-    const int step = FEW_WAVES * BLOCK;
-    int x = v0 + wave * BLOCK;
-    Entry next = entry_of(a.rows, b, key_at(keys, min(x + (lane & 31), keys.n - 1)));
-    for (; x < v1; x += step) {
-        const Spot spot = spot_of(a.rows, next);
-        next = entry_of(a.rows, b, key_at(keys, min(x + step + (lane & 31), keys.n - 1)));
-        const int64_t off = spot_bytes(a, spot);
-        const unsigned lost = (unsigned)__builtin_amdgcn_ballot_w64(spot.page < 0);   // keys without a page
-        int ke = 0, ve = 0;
-        if constexpr (F8) {
-            const int64_t at = spot_exp(a, spot, hkv);
-            ke = a.k_exp[at], ve = a.v_exp[at];
-        }
-        u32x4 kk[2][KL], vv[VL];
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const unsigned char *row = kb + lane_value(off, y * 16 + col) + grp * 16;
-#pragma unroll
-            for (int s = 0; s < KL; ++s) kk[y][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(row + s * 64));
-        }
-#pragma unroll
-        for (int u = 0; u < VL; ++u)
-            vv[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(vb + lane_value(off, u * RPW + lane / LPR) + lane % LPR * 16));
-
-        bool whole = lost == 0;
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) whole &= seen[cb].sees_all(x, x + BLOCK);
-        whole = __builtin_amdgcn_ballot_w64(!whole) == 0;
-
-        f32x4 acc[2][CB];
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const float scale = F8 ? power_of_two(__shfl(ke, y * 16 + col)) : 1.f;
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb) acc[y][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < KL; ++s) {
-                u32x4 ka[F8 ? 2 : 1];
-                as_bf16<F8>(kk[y][s], scale, ka);
-#pragma unroll
-                for (int z = 0; z < (F8 ? 2 : 1); ++z)
-#pragma unroll
-                    for (int cb = 0; cb < CB; ++cb)
-                        acc[y][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka[z]), q[cb][F8 ? 2 * s + z : s], acc[y][cb], 0, 0, 0);
-            }
-        }
-        bool odd = false;   // elements were taken out
-#pragma unroll
-        for (int u = 0; u < VL; ++u) {
-            u32x4 y[F8 ? 2 : 1];
-            const int row = u * RPW + lane / LPR;
-            as_bf16<F8>(vv[u], F8 ? power_of_two(__shfl(ve, row)) : 1.f, y);
-#pragma unroll
-            for (int z = 0; z < (F8 ? 2 : 1); ++z) {
-                if (!whole) odd |= take_out(y[z]);
-                const int piece = lane % LPR * (F8 ? 2 : 1) + z;
-                *reinterpret_cast<u32x4 *>(vt + row * (D * 2) + ((piece ^ few_swz<D>(row)) << 4)) = y[z];
-            }
-        }
-        odd = __builtin_amdgcn_ballot_w64(odd) != 0;
-
-        bf16x8 p[CB];
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            float s[8], mx = LOWEST;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                s[e] = acc[e / 4][cb][e % 4] * a.score_scale;
-                if (!whole) {
-                    const int key = (e / 4) * 16 + grp * 4 + e % 4;
-                    const float lost_or_not = (lost >> key) & 1 ? __builtin_nanf("") : s[e];
-                    s[e] = seen[cb].sees(x + key) ? lost_or_not : -INFINITY;
-                }
-                mx = fmaxf(mx, s[e]);
-            }
-            if (__builtin_amdgcn_ballot_w64(mx > m_run[cb]) != 0) {
-                mx = fmaxf(mx, swap16(mx));
-                mx = fmaxf(fmaxf(mx, swap32(mx)), m_run[cb]);
-                const float alpha = __builtin_amdgcn_exp2f(m_run[cb] - mx);
-                m_run[cb] = mx, l_run[cb] *= alpha;
-#pragma unroll
-                for (int db = 0; db < DB; ++db) o[cb][db] *= alpha;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float w = __builtin_amdgcn_exp2f(s[e] - m_run[cb]);
-                l_run[cb] += w;
-                p[cb][e] = (__bf16)w;
-            }
-        }
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            const unsigned char *at = vt + (t_at ^ (db << 5));
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(at));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(at + 16 * D * 2));
-            const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb) o[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p[cb], o[cb][db], 0, 0, 0);
-        }
-        if (odd) {
-#pragma unroll 1
-            for (int key = 0; key < BLOCK; ++key) {
-                const Spot at = {__builtin_amdgcn_readlane(spot.page, key), __builtin_amdgcn_readlane(spot.slot, key)};
-#pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    float y[4];
-                    no_numbers<F8>(a, hkv, at, db * 16 + grp * 4, y);
-#pragma unroll
-                    for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[cb][db][e] += seen[cb].sees(x + key) ? y[e] : 0.f;
-                }
-            }
-        }
-    }
-
-    // ---- the waves' results ------------------------------------------------------------------------------------------
-    float *const sh_o = reinterpret_cast<float *>(lds);
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        float l = l_run[cb];
-        l += swap16(l), l += swap32(l);
-        if (grp == 0) sh_m[wave][cb * 16 + col] = m_run[cb], sh_l[wave][cb * 16 + col] = l;
-        __syncthreads();   // (the V blocks, or the results of the columns before, have been read)
-#pragma unroll
-        for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(sh_o + (wave * 16 + col) * OUT_ROW + db * 16 + grp * 4) = o[cb][db];
-        __syncthreads();
-        constexpr int EACH = D / 16;
-        const int c = tid / 16, d0 = tid % 16 * EACH, pair = cb * 16 + c;
-        if (pair < pairs) {
-            float M = sh_m[0][pair];
-#pragma unroll
-            for (int y = 1; y < FEW_WAVES; ++y) M = fmaxf(M, sh_m[y][pair]);
-            float den = 0.f, out[EACH];
-#pragma unroll
-            for (int e = 0; e < EACH; ++e) out[e] = 0.f;
-#pragma unroll
-            for (int y = 0; y < FEW_WAVES; ++y) {
-                const float w = __builtin_amdgcn_exp2f(sh_m[y][pair] - M);
-                den += sh_l[y][pair] * w;
-#pragma unroll
-                for (int e = 0; e < EACH; ++e) out[e] += sh_o[(y * 16 + c) * OUT_ROW + d0 + e] * w;
-            }
-            const int row = seq.first + ksa_div(pair, a.by_group), h = hkv * a.group + pair - ksa_div(pair, a.by_group) * a.group;
-            if (a.n_splits == 1) {
-                typedef __bf16 bf16_each __attribute__((ext_vector_type(EACH)));
-                bf16_each r;
-#pragma unroll
-                for (int e = 0; e < EACH; ++e) r[e] = (__bf16)(out[e] / den);
-                *reinterpret_cast<bf16_each *>(a.o + row * a.o_row + h * a.o_head + d0) = r;
-                if (a.lse && d0 == 0) a.lse[(int64_t)row * a.n_q_heads + h] = log_sum(M, den);
-            } else {
-                float *rec = a.ws + (((int64_t)row * a.n_q_heads + h) * a.n_splits + split) * OUT_ROW;
-#pragma unroll
-                for (int e = 0; e < EACH; e += 4) *reinterpret_cast<f32x4 *>(rec + d0 + e) = f32x4{out[e], out[e + 1], out[e + 2], out[e + 3]};
-                if (d0 == 0) rec[D] = M, rec[D + 1] = den;
-            }
-        }
-    }
-}
-
-// ---- many rows ----------------------------------------------------------------------------------------------------------
-
-constexpr int BN = 64;   // keys of a tile
 // A row's weights go by a reference that is one of its scores, not the largest: no weight is too small to count, and the sum of 16 of them is
 // looked at instead of their scores.  Above this a new reference is taken and the 16 are worked out again.
 constexpr float HIGH = 1048576.f;
-#define KSA_FENCE() __builtin_amdgcn_sched_barrier(0)
 
 // Bytes from one row of a tile to the next in LDS: the 16 rows of a phase of the plain reads of K, 16 bytes each, and the 4 rows of one of the
 // transposing reads of V, 64 bytes each, lie in different banks, and every address is a base plus a constant.
@@ -353,18 +131,238 @@ struct TileRow {
     static constexpr int K = D * 2 + 16, V = D * 2 + 64;
 };
 
-// Bytes of an 8-bit word (halves of a word of bf16) that are no numbers become zero; whether there were any.
-template <bool F8>
-__device__ __forceinline__ bool take_out_raw(u32x4 &x) {
-    if constexpr (!F8) return take_out(x);
-    unsigned any = 0;
+// Sixteen weights of a lane that sum up to more than HIGH: the row's reference becomes the largest of its scores, what has been summed follows.
+template <int DB>
+__device__ __forceinline__ float raised(const f32x16 &sc, float sum, float m_run, float scale, float &l_run, f32x16 (&o)[DB]) {
+    float most = sc[0];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const unsigned hit = ((x[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // (0x7f and 0xff are the NaNs)
-        any |= hit, x[e] &= ~((hit >> 7) * 0xffu);
-    }
-    return any != 0;
+    for (int g = 1; g < 16; ++g) most = fmaxf(most, sc[g]);
+    most = fmaxf(most, swap32(most)) * scale;
+    const float m = fmaxf(sum, swap32(sum)) > HIGH ? fmaxf(most, m_run) : m_run;   // (by the row alone)
+    const float alpha = __builtin_amdgcn_exp2f(m_run - m);
+    l_run *= alpha;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 16; ++g) o[db][g] *= alpha;
+    return m;
 }
+// The elements of a V row that are no numbers, to the output of a row that sees it.
+template <int D, bool F8>
+__device__ __forceinline__ void add_no_numbers(const FwdArgs &a, int hkv, const Spot &at, int h, bool see, f32x16 (&o)[D / 32]) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            float z[4];
+            no_numbers<F8>(a, hkv, at, db * 32 + 8 * g + 4 * h, z);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[db][4 * g + e] += see ? z[e] : 0.f;
+        }
+}
+
+// ---- few rows -----------------------------------------------------------------------------------------------------------
+
+// At most 32 pairs.  Every wave has blocks of 32 keys of its own, in LDS of its own: no barriers before the end.  The rows of the next block are
+// on their way while one is worked on.
+constexpr int FEW_WAVES = 4, BLOCK = 32;
+
+template <int D, bool F8>
+__global__ __launch_bounds__(FEW_WAVES * 64, 2) void ksa_paged_few_kernel(const FwdArgs a) {
+    constexpr int KS = D / 16, DB = D / 32, ES = F8 ? 1 : 2;
+    constexpr int LPR = D * ES / 16, RPI = 64 / LPR, NI = BLOCK / RPI;   // lanes per row, rows per load, loads per tensor
+    constexpr int KROW = TileRow<D>::K, VROW = TileRow<D>::V, OWN = BLOCK * (KROW + VROW), OUT_ROW = D + 4;
+    static_assert(BLOCK * OUT_ROW * 4 <= OWN, "a wave's results lie where its blocks were");
+    __shared__ __align__(16) unsigned char lds[FEW_WAVES * OWN];
+    __shared__ float sh_m[FEW_WAVES][32], sh_l[FEW_WAVES][32];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 31, h = lane >> 5;
+    const int split = blockIdx.x, hkv = blockIdx.y, b = blockIdx.z;
+    const NewRows seq = new_rows(a.rows, b, a.max_rows);
+    if (seq.n == 0) return;
+    if (!seq.ok) {
+        if (a.n_splits > 1) return;   // (the joining kernel sees to it)
+        for (int x = tid; x < seq.n * a.group * D; x += FEW_WAVES * 64) {
+            const int row = x / (a.group * D), hq = hkv * a.group + x / D % a.group;
+            a.o[(seq.first + row) * a.o_row + hq * a.o_head + x % D] = (__bf16)__builtin_nanf("");
+            if (a.lse && x % D == 0) a.lse[(int64_t)(seq.first + row) * a.n_q_heads + hq] = __builtin_nanf("");
+        }
+        return;
+    }
+    const Keys keys = keys_of(a.rows, seq.start, seq.start + seq.n - 1);
+    const int per = ksa_div((keys.n + BLOCK - 1) / BLOCK + a.n_splits - 1, a.by_splits) * BLOCK;
+    const int v0 = split * per, v1 = min(keys.n, v0 + per);
+
+    // ---- blocks on their way: table entries two ahead, rows into registers one ahead, as bf16 into LDS ----------------------
+    const unsigned char *const kb = a.k + hkv * a.head_bytes, *const vb = a.v + hkv * a.head_bytes;
+    const int f_row = lane / LPR, f_piece = lane % LPR;
+    u32x4 kr[NI], vr[NI];
+    int ke = 0, ve = 0;        // exponents of row lane % 32
+    unsigned lost = 0;         // keys without a page
+    // Loads return in the order they are issued in: a block's table entries are asked for before the rows of the block in front of it.
+    Entry entry;               // of row lane % 32 of the block to be requested next
+    auto look = [&](int x) { return entry_of(a.rows, b, key_at(keys, min(x + r, keys.n - 1))); };
+    auto request = [&](int x_next) {
+        const Spot spot = spot_of(a.rows, entry);
+        entry = look(x_next);
+        const int64_t off = spot_bytes(a, spot);
+        lost = (unsigned)__builtin_amdgcn_ballot_w64(spot.page < 0);
+        if constexpr (F8) {
+            const int64_t at = spot_exp(a, spot, hkv);
+            ke = a.k_exp[at], ve = a.v_exp[at];
+        }
+        int64_t from[NI];
+#pragma unroll
+        for (int i = 0; i < NI; ++i) from[i] = lane_value(off, i * RPI + f_row) + f_piece * 16;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) kr[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kb + from[i]));
+#pragma unroll
+        for (int i = 0; i < NI; ++i) vr[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(vb + from[i]));
+    };
+    constexpr int STEP = FEW_WAVES * BLOCK;
+    const int first = v0 + wave * BLOCK;
+    if (first < v1) {
+        entry = look(first);
+        request(first + STEP);
+    }
+
+    // the lane's pair = row * group + head (the last one repeats)
+    const int pairs = seq.n * a.group, pair = min(r, pairs - 1), q_row = ksa_div(pair, a.by_group), q_head = hkv * a.group + pair - q_row * a.group;
+    const Seen seen = seen_of(keys, visible(a.rows, kind_of(a.rows, seq.start + q_row)));
+    bf16x8 q[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) q[s] = scaled_q(a.q + (seq.first + q_row) * a.q_row + q_head * a.q_head + s * 16 + h * 8, a.q_scale);
+
+    f32x16 o[DB];
+    float m_run = LOWEST, l_run = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 16; ++g) o[db][g] = 0.f;
+    unsigned char *const own = lds + wave * OWN;
+    const int grp = lane >> 4, li = lane & 15;
+    const unsigned char *const k_at = own + r * KROW + h * 16, *const v_at = own + BLOCK * KROW + (4 * (grp >> 1) + (li >> 2)) * VROW + 32 * (grp & 1) + 8 * (li & 3);
+    unsigned char *const put_k_at = own + f_row * KROW + f_piece * (F8 ? 32 : 16), *const put_v_at = own + BLOCK * KROW + f_row * VROW + f_piece * (F8 ? 32 : 16);
+    auto put = [&](const u32x4 &x, int e, int i, unsigned char *to) {
+        u32x4 y[F8 ? 2 : 1];
+        as_bf16<F8>(x, F8 ? power_of_two(__shfl(e, i * RPI + f_row)) : 1.f, y);
+#pragma unroll
+        for (int z = 0; z < (F8 ? 2 : 1); ++z) *reinterpret_cast<u32x4 *>(to + z * 16) = y[z];
+    };
+    auto sees_all = [&](int x) { return __builtin_amdgcn_ballot_w64(!seen.sees_all(x, x + BLOCK)) == 0; };
+    bool ever = false;         // elements of V were taken out
+    for (int x = first; x < v1; x += STEP) {
+        const unsigned none = lost;
+        const bool whole = none == 0 && sees_all(x);
+        if (!whole) {
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) odd |= take_out_raw<F8>(vr[i]);
+            ever |= __builtin_amdgcn_ballot_w64(odd) != 0;
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) put(kr[i], ke, i, put_k_at + i * RPI * KROW);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) put(vr[i], ve, i, put_v_at + i * RPI * VROW);
+        if (x + STEP < v1) request(x + 2 * STEP);
+
+        f32x16 sc;
+#pragma unroll
+        for (int g = 0; g < 16; ++g) sc[g] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(k_at + s * 32), q[s], sc, 0, 0, 0);
+        if (!whole) {
+#pragma unroll
+            for (int g = 0; g < 16; ++g) {
+                const int key = 8 * (g / 4) + 4 * h + g % 4;
+                const float lost_or_not = (none >> key) & 1 ? __builtin_nanf("") : sc[g];
+                sc[g] = seen.sees(x + key) ? lost_or_not : -INFINITY;
+            }
+        }
+        bf16x8 p[2];
+        float sum = 0.f;
+        auto weights = [&]() {
+            sum = 0.f;
+#pragma unroll
+            for (int g = 0; g < 16; ++g) {
+                const float w = __builtin_amdgcn_exp2f(fmaf(sc[g], a.score_scale, -m_run));
+                sum += w, p[g / 8][g % 8] = (__bf16)w;
+            }
+        };
+        weights();
+        if (__builtin_amdgcn_ballot_w64(sum > HIGH) != 0) {
+            m_run = raised(sc, sum, m_run, a.score_scale, l_run, o);
+            weights();
+        }
+        l_run += sum;
+#pragma unroll
+        for (int y = 0; y < 2 * DB; ++y) {   // 16 keys y / DB, columns 32 (y % DB) ..
+            const unsigned char *at = v_at + y / DB * 16 * VROW + y % DB * 64;
+            const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(at));
+            const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(at + 8 * VROW));
+            const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+            o[y % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[y / DB], o[y % DB], 0, 0, 0);
+        }
+    }
+    if (ever) {   // what was taken out of V, to the rows that see it
+        for (int x = first; x < v1; x += STEP)
+            for (int key = 0; key < min(BLOCK, keys.n - x); ++key) {
+                const Spot at = spot_of(a.rows, entry_of(a.rows, b, key_at(keys, x + key)));
+                if (sees_all(x) && at.page >= 0) continue;   // (where a page is missing the sum is none anyway)
+                add_no_numbers<D, F8>(a, hkv, at, h, seen.sees(x + key), o);
+            }
+    }
+
+    // ---- the waves' results ------------------------------------------------------------------------------------------
+    const float l = l_run + swap32(l_run);
+    if (h == 0) sh_m[wave][r] = m_run, sh_l[wave][r] = l;
+    float *const mine = reinterpret_cast<float *>(own);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<f32x4 *>(mine + r * OUT_ROW + db * 32 + 8 * g + 4 * h) = f32x4{o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]};
+    __syncthreads();
+    constexpr int LANES = D / 8;   // lanes per pair
+#pragma unroll
+    for (int x = tid / LANES; x < 32; x += FEW_WAVES * 64 / LANES) {
+        if (x >= pairs) break;
+        const int d0 = tid % LANES * 8;
+        float M = sh_m[0][x];
+#pragma unroll
+        for (int y = 1; y < FEW_WAVES; ++y) M = fmaxf(M, sh_m[y][x]);
+        float den = 0.f, out[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[e] = 0.f;
+#pragma unroll
+        for (int y = 0; y < FEW_WAVES; ++y) {
+            const float w = __builtin_amdgcn_exp2f(sh_m[y][x] - M);
+            const float *from = reinterpret_cast<const float *>(lds + y * OWN) + x * OUT_ROW + d0;
+            den += sh_l[y][x] * w;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) out[e] += from[e] * w;
+        }
+        const int row = seq.first + ksa_div(x, a.by_group), hq = hkv * a.group + x - ksa_div(x, a.by_group) * a.group;
+        if (a.n_splits == 1) {
+            bf16x8 z;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = (__bf16)(out[e] / den);
+            *reinterpret_cast<bf16x8 *>(a.o + row * a.o_row + hq * a.o_head + d0) = z;
+            if (a.lse && d0 == 0) a.lse[(int64_t)row * a.n_q_heads + hq] = log_sum(M, den);
+        } else {
+            float *rec = a.ws + (((int64_t)row * a.n_q_heads + hq) * a.n_splits + split) * OUT_ROW;
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) *reinterpret_cast<f32x4 *>(rec + d0 + e) = f32x4{out[e], out[e + 1], out[e + 2], out[e + 3]};
+            if (d0 == 0) rec[D] = M, rec[D + 1] = den;
+        }
+    }
+}
+
+// ---- many rows ----------------------------------------------------------------------------------------------------------
+
+constexpr int BN = 64;   // keys of a tile
+#define KSA_FENCE() __builtin_amdgcn_sched_barrier(0)
 
 // What a workgroup works on: pairs [first, first + PAIRS) of sequence b's new text rows (or summary rows), p = row * group + head.
 struct Tile {
@@ -612,17 +610,8 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
         weight(2 * KS), weight(2 * KS + 1);
         if constexpr (WEIGHTS) {
             if (__builtin_amdgcn_ballot_w64(sum > HIGH) != 0) {
-                float most = sc[y ^ 1][0];
-#pragma unroll
-                for (int g = 1; g < 16; ++g) most = fmaxf(most, sc[y ^ 1][g]);
-                most = fmaxf(most, swap32(most)) * a.score_scale;
-                const float m = fmaxf(sum, swap32(sum)) > HIGH ? fmaxf(most, m_run) : m_run;   // (by the row alone)
-                const float alpha = __builtin_amdgcn_exp2f(m_run - m);
-                m_run = m, l_run *= alpha, sum = 0.f;
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-#pragma unroll
-                    for (int g = 0; g < 16; ++g) o[db][g] *= alpha;
+                m_run = raised(sc[y ^ 1], sum, m_run, a.score_scale, l_run, o);
+                sum = 0.f;
 #pragma unroll
                 for (int g = 0; g < 16; ++g) {
                     const float w = __builtin_amdgcn_exp2f(fmaf(sc[y ^ 1][g], a.score_scale, -m_run));
@@ -718,16 +707,7 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
 #pragma unroll 1
         for (int x = first_tile * BN; x < min(end_tile * BN, keys.n); ++x) {
             if (tile_all.sees_all(x / BN * BN, x / BN * BN + BN)) continue;
-            const Spot sp = spot_of(a.rows, entry_of(a.rows, tile.b, key_at(keys, x)));
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    float z[4];
-                    no_numbers<F8>(a, hkv, sp, db * 32 + 8 * g + 4 * h, z);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[db][4 * g + e] += seen.sees(x) ? z[e] : 0.f;
-                }
+            add_no_numbers<D, F8>(a, hkv, spot_of(a.rows, entry_of(a.rows, tile.b, key_at(keys, x))), h, seen.sees(x), o);
         }
     }
     const float l = l_run + swap32(l_run);
@@ -768,57 +748,83 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
     }
 }
 
-// ---- the spans' records of one (row, query head) joined, one wave each ------------------------------------------------------
+// ---- the spans' records joined by log-sum-exp -------------------------------------------------------------------------------
 
-template <int D>
+// PARTS waves per (row, query head), each with every PARTS-th group of 8 spans, whose loads travel together; the weights of 64 spans live in
+// the lanes of every wave.
+template <int D, int PARTS>
 __global__ __launch_bounds__(256) void ksa_paged_join_kernel(const FwdArgs a) {
-    constexpr int EACH = D / 64;
-    const int lane = threadIdx.x & 63;
-    const int64_t x = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row = (int)(x / a.n_q_heads), hq = (int)(x - (int64_t)row * a.n_q_heads);
-    if (row >= a.rows.total) return;
-    const int b = sequence_of(a.rows, row);
-    if (b == a.rows.batch) return;
-    const NewRows seq = new_rows(a.rows, b, a.max_rows);
-    if (row < seq.first || row >= seq.first + seq.n) return;
-    float out[EACH], M = LOWEST, den = 0.f;
+    constexpr int EACH = D / 64, REC = D + 4, ITEMS = 4 / PARTS, MU = 8;
+    typedef float each __attribute__((ext_vector_type(EACH)));
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = wave % PARTS;
+    const int item = blockIdx.x * ITEMS + wave / PARTS;   // row * n_q_heads + query head
+    const int row = ksa_div(item, a.by_q_heads), hq = item - row * a.n_q_heads;
+    NewRows seq = {0, 0, 0, false};
+    if (row < a.rows.total) {
+        const int b = sequence_of(a.rows, row);
+        if (b < a.rows.batch) seq = new_rows(a.rows, b, a.max_rows);
+    }
+    const bool any = row >= seq.first && row < seq.first + seq.n;
+    each out;
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) out[e] = __builtin_nanf("");
-    if (seq.ok) {
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) out[e] = 0.f;
-        const float *rec = a.ws + x * a.n_splits * (D + 4);
-        for (int s = lane; s < a.n_splits; s += 64) M = fmaxf(M, rec[(int64_t)s * (D + 4) + D]);
+    for (int e = 0; e < EACH; ++e) out[e] = 0.f;
+    float M = LOWEST, den = 0.f;
+    if (any && seq.ok) {
+        const int n = a.n_splits;
+        const float *const rec = a.ws + (int64_t)item * n * REC;
+        auto at = [&](int s) { return rec + (int64_t)min(s, n - 1) * REC; };
+        float m = at(lane)[D], l = lane < n ? at(lane)[D + 1] : 0.f;
+        M = m;
+        for (int s = 64; s < n; s += 64) M = fmaxf(M, at(s + lane)[D]);
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
-        for (int s = 0; s < a.n_splits; ++s) {
-            const float *at = rec + (int64_t)s * (D + 4);
-            const float w = __builtin_amdgcn_exp2f(at[D] - M);
-            den += at[D + 1] * w;
+        for (int s = 0; s < n; s += 64) {
+            if (s > 0) m = at(s + lane)[D], l = s + lane < n ? at(s + lane)[D + 1] : 0.f;
+            const float w = __builtin_amdgcn_exp2f(m - M);
+            den += l * w;
+            for (int x = MU * part; x < min(64, n - s); x += MU * PARTS) {
+                each o[MU];
 #pragma unroll
-            for (int e = 0; e < EACH; ++e) out[e] += at[lane * EACH + e] * w;
+                for (int u = 0; u < MU; ++u) o[u] = *reinterpret_cast<const each *>(at(s + x + u) + lane * EACH);
+#pragma unroll
+                for (int u = 0; u < MU; ++u)
+                    if (s + x + u < n) out += o[u] * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), x + u));
+            }
         }
-    } else {
-        den = __builtin_nanf("");
-    }
-    __bf16 *to = a.o + row * a.o_row + hq * a.o_head + lane * EACH;
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) to[e] = (__bf16)(out[e] / den);
-    if (a.lse && lane == 0) a.lse[x] = log_sum(M, den);
+        for (int d = 32; d > 0; d >>= 1) den += __shfl_xor(den, d);
+    }
+    if constexpr (PARTS > 1) {
+        __shared__ each parts[4][64];
+        parts[wave][lane] = out;
+        __syncthreads();
+        if (part > 0) return;
+#pragma unroll
+        for (int y = 1; y < PARTS; ++y) out += parts[wave + y][lane];
+    }
+    if (!any) return;
+    if (!seq.ok) den = __builtin_nanf("");
+    typedef __bf16 each_bf16 __attribute__((ext_vector_type(EACH)));
+    each_bf16 r;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) r[e] = (__bf16)(out[e] / den);
+    *reinterpret_cast<each_bf16 *>(a.o + row * a.o_row + hq * a.o_head + lane * EACH) = r;
+    if (a.lse && lane == 0) a.lse[item] = log_sum(M, den);
 }
 
 template <int D, bool F8>
 void launch(const FwdArgs &a, const KsaPagedPlan &plan, hipStream_t st) {
     const dim3 few(plan.n_splits, a.n_kv_heads, a.rows.batch);
-    if (plan.columns == 16) hipLaunchKernelGGL((ksa_paged_few_kernel<D, F8, 16>), few, dim3(FEW_WAVES * 64), 0, st, a);
-    else if (plan.columns == 32) hipLaunchKernelGGL((ksa_paged_few_kernel<D, F8, 32>), few, dim3(FEW_WAVES * 64), 0, st, a);
+    if (plan.few) hipLaunchKernelGGL((ksa_paged_few_kernel<D, F8>), few, dim3(FEW_WAVES * 64), 0, st, a);
     else {
         const dim3 many((unsigned)(plan.slots * plan.n_splits * a.n_kv_heads));
         if (plan.pairs == 128) hipLaunchKernelGGL((ksa_paged_many_kernel<D, F8, 4>), many, dim3(256), 0, st, a);
         else hipLaunchKernelGGL((ksa_paged_many_kernel<D, F8, 8>), many, dim3(512), 0, st, a);
     }
-    if (plan.n_splits > 1)
-        hipLaunchKernelGGL((ksa_paged_join_kernel<D>), dim3((unsigned)(((int64_t)a.rows.total * a.n_q_heads + 3) / 4)), dim3(256), 0, st, a);
+    if (plan.n_splits == 1) return;
+    const int items = a.rows.total * a.n_q_heads;
+    if (plan.n_splits > 8) hipLaunchKernelGGL((ksa_paged_join_kernel<D, 4>), dim3(items), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((ksa_paged_join_kernel<D, 1>), dim3((items + 3) / 4), dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -835,7 +841,7 @@ int ksa_launch_paged_fwd(const KsaPagedFwd &L, void *stream) {
     a.max_rows = L.max_rows;
     a.n_q_heads = p.n_q_heads, a.n_kv_heads = p.n_kv_heads, a.group = p.n_q_heads / p.n_kv_heads;
     a.n_splits = L.plan.n_splits;
-    a.by_group = ksa_divisor(a.group), a.by_heads = ksa_divisor(a.n_kv_heads), a.by_splits = ksa_divisor(a.n_splits);
+    a.by_group = ksa_divisor(a.group), a.by_heads = ksa_divisor(a.n_kv_heads), a.by_splits = ksa_divisor(a.n_splits), a.by_q_heads = ksa_divisor(a.n_q_heads);
     // With the first factor in q the products are no larger than the scaled scores and at least half as large, so that they do not
     // overflow where those would not.
     const float scale = p.softmax_scale * 1.4426950408889634f;

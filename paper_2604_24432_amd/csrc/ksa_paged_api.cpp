@@ -1,5 +1,6 @@
 // C-ABI entry points of the paged cache.  Every argument check happens before the first HIP call.
 #include <algorithm>
+#include <cmath>
 
 #include "ksa_internal.h"
 #include "ksa_paged.h"
@@ -59,30 +60,57 @@ int check_strides(int64_t out[2], const int64_t *given, int32_t heads, int32_t h
     return out[0] > 0 && out[1] > 0 && out[0] % 8 == 0 && out[1] % 8 == 0 ? KSA_OK : KSA_ERR_INVALID_ARG;
 }
 
-// Keys that a sequence's rows see together, none less: the summaries, the text of the window and of the new rows.
-int64_t most_keys(const ksa_params *p, int64_t max_rows) {
-    const int64_t text = std::min<int64_t>(p->n_text, (int64_t)p->window_chunks * p->chunk_len + p->chunk_len + max_rows);
+// Keys that so many consecutive rows of a sequence see together, none less: the summaries, the text of the window and of the rows.
+int64_t most_keys(const ksa_params *p, int64_t rows) {
+    const int64_t text = std::min<int64_t>(p->n_text, (int64_t)p->window_chunks * p->chunk_len + p->chunk_len + rows);
     return (int64_t)(p->n_text / p->chunk_len) * p->n_summary + text;
 }
 
+/*
+ * How a call is dealt.  All times in us.
+ *
+ * Few rows: a workgroup per sequence, KV head and span of the keys, about 512 of them (two on each compute unit) and no span below 256 keys, 512 with
+ * many sequences and heads.  32 of these, 4200 keys, 32/8 heads: 4 spans 21.5, 8 17.6, 16 17.2, 32 21.9; 128, 9000 keys, 8 rows, 8-bit: 2 78.5, 4 53.1,
+ * 8 52.3, 16 58.1; 256, 4000 keys, 16/16 heads 1 57.6, 2 57.2, 4 55.9; 512, 16500 keys 1 636, 2 641, 4 656; 16, 65536 keys, 8 rows 8 99, 16 89, 32 91; 160,
+ * 800 keys 1 13.6, 3 15.0.  Spans dealt by the sequences' lengths (lengths 1 : 4): 128 57.4, the same number each 53.8; 512 248, 249.
+ *
+ * Many rows: tiles of 128 pairs, two on a compute unit, or of 256, which take their keys from memory half as often but fill a unit alone.  Tiles
+ * and spans are chosen by what they are expected to take: a start and an end, the key tiles of a span one after the other, rounds where there are
+ * more workgroups than places, and for the records of several spans a second kernel.  Per key tile of head_dim 128: 128 pairs 1.6 alone on a unit, 2.1 in
+ * pairs, 256 pairs 1.95.  Expected / measured: full attention, 2048 rows, 64K keys, 32/8 heads 256 pairs 2005 / 2020, 128 2157 / 2194; 512 rows 128
+ * pairs in 4 spans 554 / 585, in 8 574 / 618, in 3 631 / 656; 8 x 100 rows, 4200 keys 2 spans 77 / 75, 3 71 / 61, 1 112 / 109; window of 1023, 1280 rows, 16/16
+ * heads 1 span 34 / 38, 2 38 / 46; 2595 rows of six sequences, 2700 keys, 12/4 heads, head_dim 64 1 48 / 56, 2 37 / 48, 4 42 / 53; 64 rows, 830 keys,
+ * 8/4 heads 1 18 / 23, 4 12 / 15, 8 11 / 12.
+ */
 KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_rows, int32_t n_splits) {
     const int32_t group = p->n_q_heads / p->n_kv_heads;
-    KsaPagedPlan plan = {0, 1, 0, 0};
-    const int64_t pairs = max_rows * group, keys = most_keys(p, max_rows);
-    int64_t units, want, least;   // workgroups of one span; how many are wanted; keys of a span
-    if (pairs <= 32) {
-        plan.columns = pairs <= 16 ? 16 : 32;
-        units = (int64_t)p->batch * p->n_kv_heads, want = 1024, least = 256;
-    } else {
-        // Tiles of 256 pairs take their keys from memory half as often, but fill a compute unit alone: where there are as many as units
-        // (full attention, 2048 rows, 64K keys, 32/8 heads: 128 pairs 2194 us, 256 2020; 8-bit, 4608 rows, 128K 1095, 1017; window of 1023, 1280
-        // rows, 16/16 heads 43, 56).  Every sequence ends one tile of text and one of summaries before it is full.
-        plan.pairs = total_rows * p->n_q_heads >= 256 * 256 ? 256 : 128;
-        plan.slots = (int32_t)((total_rows * group) / plan.pairs + (p->n_summary > 0 ? 2 : 1) * (int64_t)p->batch);
-        units = (int64_t)plan.slots * p->n_kv_heads, want = plan.pairs == 256 ? 256 : 512, least = 512;
+    KsaPagedPlan plan = {false, n_splits, 0, 0};
+    if (max_rows * group <= KSA_PAGED_FEW) {
+        plan.few = true;
+        const int64_t units = (int64_t)p->batch * p->n_kv_heads;
+        if (n_splits != 0) return plan;
+        const int64_t keys = most_keys(p, max_rows);
+        plan.n_splits = (int32_t)std::max<int64_t>(1, std::min({512 / units, keys / (units >= 128 ? 512 : 256), (int64_t)64}));
+        return plan;
     }
-    plan.n_splits = n_splits;
-    if (n_splits == 0) plan.n_splits = (int32_t)std::max<int64_t>(1, std::min({want / units, keys / least, (int64_t)64}));
+    const double size = p->head_dim == 128 ? 1.0 : 0.62;
+    const double records = 8e-7 * (double)total_rows * p->n_q_heads * ksa_paged_record(p->head_dim);   // written and read, of one span
+    double best = 0;
+    for (const int32_t pairs : {128, 256}) {
+        // every sequence ends one tile of text and one of summaries before it is full; the latter's lists are short
+        const int64_t slots = total_rows * group / pairs + (p->n_summary > 0 ? 2 : 1) * (int64_t)p->batch;
+        const double rows = (double)total_rows * p->chunk_len / (p->chunk_len + p->n_summary);
+        const double units = (rows * group / pairs + 0.5 * p->batch) * p->n_kv_heads;
+        const int64_t tiles = (most_keys(p, std::min<int64_t>(max_rows, pairs / group + 1)) + 63) / 64;
+        for (int32_t n = n_splits == 0 ? 1 : n_splits; n <= (n_splits == 0 ? 64 : n_splits); ++n) {
+            if (n_splits == 0 && n > 1 && n > tiles) break;
+            const double places = pairs == 128 ? 512 : 256, wgs = units * n;
+            const double tile = size * (pairs == 256 ? 1.95 : 1.6 + 0.5 * std::min(std::max((wgs - 256) / 256, 0.0), 1.0));
+            const double rounds = std::max(1.0, 0.7 * wgs / places + 0.3 * std::ceil(wgs / places));   // (workgroups of different lengths)
+            const double time = rounds * (5 + (double)((tiles + n - 1) / n) * tile) + (n > 1 ? 3.5 + records * n : 0);
+            if (plan.slots == 0 || time < best) best = time, plan.pairs = pairs, plan.slots = (int32_t)slots, plan.n_splits = n;
+        }
+    }
     return plan;
 }
 
