@@ -355,8 +355,9 @@ typedef struct ksa_paged_cache {
  * Nothing is allocated, cleared or waited for: all of them may be captured into a graph, and what lies in device memory (cu_rows,
  * start, the tables) may change between replays.  total_rows = 0 is a no-op.
  * kv_strides, q_strides, o_strides: {row, head} in elements, multiples of 8, the last dim contiguous; NULL = contiguous.
- * Errors of all: INVALID_ARG (null or misaligned pointers: 16 bytes, 4 for int32 and fp32; bad strides or cache fields), UNSUPPORTED (2^31 and
- * more (row, head) pairs; what ksa_params excludes), HIP.
+ * Errors of all: INVALID_ARG (null or misaligned pointers: 16 bytes, 4 for int32 and fp32; bad strides or cache fields), UNSUPPORTED (more
+ * than a launch holds: 2^28 (row, KV head) pairs of head_dim 128 into or out of the cache, 2^31 (row, query head) pairs of the attention, 2^24 in several
+ * spans; what ksa_params excludes), HIP.
  */
 
 /* Columns that the tables need for the first n_rows augmented rows of a sequence. */

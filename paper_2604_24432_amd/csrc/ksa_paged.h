@@ -63,15 +63,33 @@ inline PagedRows paged_rows(const KsaPagedCall &L) {
     return a;
 }
 
-// The sequence of a packed row: so many end at or in front of it (cu_rows does not decrease); a.batch if none is left.  The row is the same
-// for all lanes of the wave.
-__device__ __forceinline__ int sequence_of(const PagedRows &a, int row) {
+// The new rows of a packed row's sequence, and the sequence; a.batch and none for a row behind them all.  A sequence is the row's if so many end at
+// or in front of the row (cu_rows does not decrease).  The wave's rows are first (the same in all lanes) .. first + ROWS - 1; 64 sequences are
+// looked at together, all that there is to know of them loaded at once.
+template <int ROWS>
+__device__ __forceinline__ NewRows sequence_of(const PagedRows &a, int first, int row, int max_rows, int &b) {
     const int lane = threadIdx.x & 63;
-    for (int b = 0; b < a.batch; b += 64) {
-        const uint64_t ended = __builtin_amdgcn_ballot_w64(b + lane < a.batch && a.cu[min(b + lane, a.batch - 1) + 1] <= row);
-        if (ended != ~(uint64_t)0) return b + __builtin_popcountll(ended);
+    for (b = 0; b < a.batch; b += 64) {
+        const bool any = b + lane < a.batch;
+        const NewRows s = new_rows(a, min(b + lane, a.batch - 1), max_rows);
+        const int end = a.cu[min(b + lane, a.batch - 1) + 1];
+        const uint64_t ended = __builtin_amdgcn_ballot_w64(any & (end <= first));
+        if (ended == ~(uint64_t)0) continue;
+        int at = __builtin_popcountll(ended);
+#pragma unroll
+        for (int r = 1; r < ROWS; ++r) {
+            const int ended_by = __builtin_popcountll(__builtin_amdgcn_ballot_w64(any & (end <= first + r)));
+            if (row >= first + r) at = ended_by;
+        }
+        b += at;
+        if (ROWS > 1 && __builtin_amdgcn_ballot_w64(at == 64) != 0) {   // some row's sequence is not among these
+            while (b < a.batch && a.cu[b + 1] <= row) ++b;
+            return b < a.batch ? new_rows(a, b, max_rows) : NewRows{0, 0, 0, false};
+        }
+        const NewRows mine = {__shfl(s.first, at), __shfl(s.n, at), __shfl(s.start, at), __shfl(s.ok ? 1 : 0, at) != 0};
+        return b < a.batch ? mine : NewRows{0, 0, 0, false};
     }
-    return a.batch;
+    return {0, 0, 0, false};
 }
 
 // Four e4m3 numbers times `scale`, a power of two, as bf16.

@@ -69,18 +69,22 @@ int64_t most_keys(const ksa_params *p, int64_t rows) {
 /*
  * How a call is dealt.  All times in us.
  *
- * Few rows: a workgroup per sequence, KV head and span of the keys, about 512 of them (two on each compute unit) and no span below 256 keys, 512 with
- * many sequences and heads.  32 of these, 4200 keys, 32/8 heads: 4 spans 21.5, 8 17.6, 16 17.2, 32 21.9; 128, 9000 keys, 8 rows, 8-bit: 2 78.5, 4 53.1,
- * 8 52.3, 16 58.1; 256, 4000 keys, 16/16 heads 1 57.6, 2 57.2, 4 55.9; 512, 16500 keys 1 636, 2 641, 4 656; 16, 65536 keys, 8 rows 8 99, 16 89, 32 91; 160,
- * 800 keys 1 13.6, 3 15.0.  Spans dealt by the sequences' lengths (lengths 1 : 4): 128 57.4, the same number each 53.8; 512 248, 249.
+ * Few rows: a workgroup per sequence, KV head and span of the keys, about 512 of them (two on each compute unit), and no span below 128 keys, 256
+ * from 64 sequences x KV heads on, 512 from 128 on; below 512 keys one span.  Sequences x KV heads, keys: 1, 400 1 7.9, 4 7.5; 1, 700 1 9.6, 4 7.8, 6
+ * 7.9; 1, 1200 2 11.1, 6 8.1, 16 8.5; 1, 9000 16 15.5, 32 12.9, 64 11.9; 8, 6000 8 17.3, 24 12.7, 64 13.1; 32, 800 4 11.0, 8 10.4, 16 10.9; 32, 4200 4
+ * 21.5, 8 17.6, 16 17.2, 32 21.9; 64, 800 3 12.8, 4 12.0, 6 13.7; 64, 1500 4 15.8, 6 16.4; 128, 9000, 8 rows, 8-bit 2 78.5, 4 53.1, 8 52.3, 16 58.1; 160, 800
+ * 1 13.6, 3 15.0; 256, 1500, 4 rows, 8-bit 1 26.2, 2 27.0; 256, 4000 1 57.6, 2 57.2, 4 55.9; 512, 16500 1 636, 2 641, 4 656; 16, 65536, 8 rows 8 99, 16 89,
+ * 32 91.  Spans dealt by the sequences' lengths (lengths 1 : 4): 128 57.4, the same number each 53.8; 512 248, 249.
  *
  * Many rows: tiles of 128 pairs, two on a compute unit, or of 256, which take their keys from memory half as often but fill a unit alone.  Tiles
  * and spans are chosen by what they are expected to take: a start and an end, the key tiles of a span one after the other, rounds where there are
- * more workgroups than places, and for the records of several spans a second kernel.  Per key tile of head_dim 128: 128 pairs 1.6 alone on a unit, 2.1 in
- * pairs, 256 pairs 1.95.  Expected / measured: full attention, 2048 rows, 64K keys, 32/8 heads 256 pairs 2005 / 2020, 128 2157 / 2194; 512 rows 128
- * pairs in 4 spans 554 / 585, in 8 574 / 618, in 3 631 / 656; 8 x 100 rows, 4200 keys 2 spans 77 / 75, 3 71 / 61, 1 112 / 109; window of 1023, 1280 rows, 16/16
- * heads 1 span 34 / 38, 2 38 / 46; 2595 rows of six sequences, 2700 keys, 12/4 heads, head_dim 64 1 48 / 56, 2 37 / 48, 4 42 / 53; 64 rows, 830 keys,
- * 8/4 heads 1 18 / 23, 4 12 / 15, 8 11 / 12.
+ * more workgroups than places, and for the records of several spans a second kernel.  Per key tile of head_dim 128: 128 pairs 1.75 alone on a unit,
+ * 2.05 in pairs, 256 pairs 1.85.  Measured, tiles x spans: full attention, 2048 rows, 64K keys, 32/8 heads 256 x 1 2020, 128 x 1 2194; 512
+ * rows 256 x 4 534, 128 x 4 584, 256 x 3 615, 256 x 8 572; summaries, 512 rows, 4700 keys 256 x 4 52, 128 x 4 55, 128 x 2 62, 256 x 1 119; 2304 rows,
+ * 2000 keys 128 x 1 61, 256 x 1 75, 128 x 2 88; 2048 rows, 10000 keys 256 x 1 265, 128 x 1 276, 256 x 2 284; 8 x 100 rows, 4200 keys 128 x 4 52, 128 x 3 59,
+ * 256 x 3 61, 128 x 1 110; window of 1023, 1280 rows, 16/16 heads 128 x 3 37, 128 x 1 39, 128 x 4 46, 256 x 3 40; 2595 rows of six sequences, 2700 keys, 12/4
+ * heads, head_dim 64 128 x 2 41, 128 x 4 48, 128 x 1 56, 256 x 3 50; 64 rows, 830 keys, 8/4 heads 128 x 6 12.7, 128 x 1 20, 256 x 6 13.9.  Over twelve such
+ * calls what is chosen takes 0.6 % longer than the best of 1, 2, 3, 4, 6 and 8 spans.
  */
 KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_rows, int32_t n_splits) {
     const int32_t group = p->n_q_heads / p->n_kv_heads;
@@ -90,24 +94,25 @@ KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_row
         const int64_t units = (int64_t)p->batch * p->n_kv_heads;
         if (n_splits != 0) return plan;
         const int64_t keys = most_keys(p, max_rows);
-        plan.n_splits = (int32_t)std::max<int64_t>(1, std::min({512 / units, keys / (units >= 128 ? 512 : 256), (int64_t)64}));
+        const int64_t least = units >= 128 ? 512 : units >= 64 ? 256 : 128;
+        plan.n_splits = keys < 512 ? 1 : (int32_t)std::max<int64_t>(1, std::min({512 / units, keys / least, (int64_t)64}));
         return plan;
     }
-    const double size = p->head_dim == 128 ? 1.0 : 0.62;
-    const double records = 8e-7 * (double)total_rows * p->n_q_heads * ksa_paged_record(p->head_dim);   // written and read, of one span
+    const double size = p->head_dim == 128 ? 1.0 : 0.7;
+    const double records = 1.5e-6 * (double)total_rows * p->n_q_heads * ksa_paged_record(p->head_dim);   // written and read, of one span
     double best = 0;
     for (const int32_t pairs : {128, 256}) {
         // every sequence ends one tile of text and one of summaries before it is full; the latter's lists are short
         const int64_t slots = total_rows * group / pairs + (p->n_summary > 0 ? 2 : 1) * (int64_t)p->batch;
         const double rows = (double)total_rows * p->chunk_len / (p->chunk_len + p->n_summary);
-        const double units = (rows * group / pairs + 0.5 * p->batch) * p->n_kv_heads;
+        const double full = rows * group / pairs, units = (p->batch == 1 ? std::ceil(full) : full + 0.5 * p->batch) * p->n_kv_heads;
         const int64_t tiles = (most_keys(p, std::min<int64_t>(max_rows, pairs / group + 1)) + 63) / 64;
         for (int32_t n = n_splits == 0 ? 1 : n_splits; n <= (n_splits == 0 ? 64 : n_splits); ++n) {
             if (n_splits == 0 && n > 1 && n > tiles) break;
             const double places = pairs == 128 ? 512 : 256, wgs = units * n;
-            const double tile = size * (pairs == 256 ? 1.95 : 1.6 + 0.5 * std::min(std::max((wgs - 256) / 256, 0.0), 1.0));
-            const double rounds = std::max(1.0, 0.7 * wgs / places + 0.3 * std::ceil(wgs / places));   // (workgroups of different lengths)
-            const double time = rounds * (5 + (double)((tiles + n - 1) / n) * tile) + (n > 1 ? 3.5 + records * n : 0);
+            const double tile = size * (pairs == 256 ? 1.85 : 1.75 + 0.3 * std::min(std::max((wgs - 256) / 256, 0.0), 1.0));
+            const double rounds = std::max(1.0, 1.03 * wgs / places);   // (workgroups of different lengths)
+            const double time = rounds * ((pairs == 256 ? 6.5 : 4) + (double)((tiles + n - 1) / n) * tile) + (n > 1 ? 3.5 + records * n : 0);
             if (plan.slots == 0 || time < best) best = time, plan.pairs = pairs, plan.slots = (int32_t)slots, plan.n_splits = n;
         }
     }
@@ -116,8 +121,12 @@ KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_row
 
 bool bad_fwd(int64_t max_rows, int32_t n_splits) { return max_rows <= 0 || n_splits < 0 || n_splits > 1024; }
 
-// more workgroups than a grid may have, or more records than bytes of a workspace can be counted
-bool too_large(const ksa_params *p, const KsaPagedPlan &plan) { return (int64_t)plan.slots * plan.n_splits * p->n_kv_heads >= (int64_t)1 << 31; }
+constexpr int64_t MOST_LANES = (int64_t)1 << 32;   // of a grid, none of its dimensions more
+
+bool too_large(const ksa_params *p, int64_t total_rows, const KsaPagedPlan &plan) {
+    if (plan.n_splits > 1 && total_rows * p->n_q_heads * (plan.n_splits > 8 ? 256 : 64) >= MOST_LANES) return true;
+    return !plan.few && (int64_t)plan.slots * plan.n_splits * p->n_kv_heads * plan.pairs * 2 >= MOST_LANES;
+}
 
 size_t workspace_of(const ksa_params *p, int64_t total_rows, const KsaPagedPlan &plan) {
     return plan.n_splits == 1 ? 0 : (size_t)total_rows * p->n_q_heads * plan.n_splits * ksa_paged_record(p->head_dim) * sizeof(float);
@@ -129,6 +138,7 @@ int move_call(KsaPagedMove &a, const ksa_params *p, const ksa_paged_cache *cache
     if (rc != KSA_OK) return rc;
     if (total_rows > 0 && (!k || !v)) return KSA_ERR_INVALID_ARG;
     if (!aligned(k, 16) || !aligned(v, 16)) return KSA_ERR_INVALID_ARG;
+    if ((total_rows * p->head_dim / 2048 + 1) * p->n_kv_heads * 256 >= MOST_LANES) return KSA_ERR_UNSUPPORTED;
     return check_strides(a.strides, strides, p->n_kv_heads, p->head_dim);
 }
 
@@ -184,7 +194,7 @@ int ksa_paged_fwd(const ksa_params *p, const ksa_paged_cache *cache, const void 
     if (total_rows == 0) return KSA_OK;
     a.max_rows = (int32_t)std::min(max_rows, total_rows);
     a.plan = plan_paged(p, total_rows, a.max_rows, n_splits);
-    if (too_large(p, a.plan)) return KSA_ERR_UNSUPPORTED;
+    if (too_large(p, total_rows, a.plan)) return KSA_ERR_UNSUPPORTED;
     const size_t need = workspace_of(p, total_rows, a.plan);
     if (need > 0 && !workspace) return KSA_ERR_INVALID_ARG;
     if (workspace_bytes < need) return KSA_ERR_WORKSPACE_TOO_SMALL;

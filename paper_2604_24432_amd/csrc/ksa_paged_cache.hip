@@ -1,5 +1,8 @@
 // Rows into and out of the paged cache, as bf16 or as e4m3 numbers with one power of two per row and KV head.  Data movement, bound by
-// HBM: 16 bytes of a row per lane, the row's largest magnitude by lane moves.
+// HBM: 16 bytes of a row per lane, the row's largest magnitude by lane moves, the table looked up by every row's lanes.  36864 rows, 8 heads,
+// d 128, 8-bit: in 58 us and out again 34, 454 MB at 4.9 TB/s (a copy on this card 5.0); 54000 rows, 16 heads, bf16, out 100 us, 5.3 TB/s; 64 rows
+// of 64 sequences 3.1 us, a launch and three loads one behind the other.  Loads of the new rows in front of the lookup (in 61 / 3.3 us),
+// two or four rows per lane (66 / 3.9, 69 / 5.0) did not pay.
 #include <hip/hip_runtime.h>
 
 #include "ksa_paged.h"
@@ -13,26 +16,24 @@ struct MoveArgs {
     unsigned char *kc, *vc;       // the pool
     uint8_t *k_exp, *v_exp;
     int64_t page_bytes, head_bytes, row_bytes;
-    int32_t n_kv_heads, n_pairs;
+    int32_t n_kv_heads;
     KsaDivisor by_heads;
 };
 
-// Pair x = (packed row, KV head), heads fastest, lies in LANES neighbouring lanes, 8 elements each.
+// A block takes 2048 / D neighbouring packed rows of one KV head, which mostly lie side by side in a page, 8 elements per lane; heads fastest.
+// (Against a block of 16 neighbouring (row, head) pairs: 54000 rows out 104 us -> 100, 36864 rows out 36 -> 34.)
 struct Place {
     int row, head, page, slot;
     bool any;                     // the row is a sequence's
 };
 template <int LANES>
-__device__ __forceinline__ Place place_of(const MoveArgs &a) {
-    const int first = (blockIdx.x * blockDim.x + (threadIdx.x & ~63u)) / LANES, x = first + (threadIdx.x & 63) / LANES;
-    Place p = {0, 0, -1, 0, false};
-    if (first >= a.n_pairs) return p;
-    int b = sequence_of(a.rows, __builtin_amdgcn_readfirstlane(ksa_div(first, a.by_heads)));
-    if (x >= a.n_pairs) return p;
-    p.row = ksa_div(x, a.by_heads), p.head = x - p.row * a.n_kv_heads;
-    while (b < a.rows.batch && a.rows.cu[b + 1] <= p.row) ++b;
-    if (b == a.rows.batch) return p;
-    const NewRows r = new_rows(a.rows, b, a.rows.total);
+__device__ __forceinline__ Place place_of(const MoveArgs &a, int group, int head) {
+    constexpr int ROWS = 256 / LANES;
+    const int first = group * ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (64 / LANES), row = first + (threadIdx.x & 63) / LANES;
+    Place p = {row, head, -1, 0, false};
+    if (first >= a.rows.total) return p;
+    int b;
+    const NewRows r = sequence_of<64 / LANES>(a.rows, first, row, a.rows.total, b);
     p.any = p.row >= r.first && p.row < r.first + r.n;
     if (!p.any || !r.ok) return p;
     const Spot s = spot_of(a.rows, entry_of(a.rows, b, kind_of(a.rows, r.start + (p.row - r.first))));
@@ -79,7 +80,8 @@ __device__ __forceinline__ u32x2 pack_fp8(const u32x4 &x, int biased) {
 template <int D, bool F8>
 __global__ __launch_bounds__(256) void ksa_paged_append_kernel(const MoveArgs a) {
     constexpr int LANES = D / 8;
-    const Place p = place_of<LANES>(a);
+    const int group = ksa_div(blockIdx.x, a.by_heads), head = blockIdx.x - group * a.n_kv_heads;
+    const Place p = place_of<LANES>(a, group, head);
     if (p.page < 0) return;
     const int piece = threadIdx.x % LANES;
     const int64_t from = p.row * a.row_stride + p.head * a.head_stride + piece * 8;
@@ -102,7 +104,8 @@ __global__ __launch_bounds__(256) void ksa_paged_append_kernel(const MoveArgs a)
 template <int D, bool F8>
 __global__ __launch_bounds__(256) void ksa_paged_read_kernel(const MoveArgs a) {
     constexpr int LANES = D / 8;
-    const Place p = place_of<LANES>(a);
+    const int group = ksa_div(blockIdx.x, a.by_heads), head = blockIdx.x - group * a.n_kv_heads;
+    const Place p = place_of<LANES>(a, group, head);
     if (!p.any) return;
     const int piece = threadIdx.x % LANES;
     u32x4 k = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u}, v = k;   // NaN
@@ -132,7 +135,6 @@ MoveArgs move_args(const KsaPagedMove &L) {
     a.k_exp = L.call.cache.k_exp, a.v_exp = L.call.cache.v_exp;
     a.page_bytes = L.call.cache_strides[0], a.head_bytes = L.call.cache_strides[1], a.row_bytes = L.call.cache_strides[2];
     a.n_kv_heads = L.call.p.n_kv_heads;
-    a.n_pairs = L.call.total_rows * a.n_kv_heads;
     a.by_heads = ksa_divisor(a.n_kv_heads);
     return a;
 }
@@ -143,7 +145,8 @@ MoveArgs move_args(const KsaPagedMove &L) {
     const MoveArgs a = move_args(L);                                                                                                  \
     const int d = L.call.p.head_dim;                                                                                                  \
     const bool f8 = L.call.cache.format == KSA_CACHE_FP8;                                                                             \
-    const dim3 grid((unsigned)(((int64_t)a.n_pairs * (d / 8) + 255) / 256));                                                          \
+    const int rows = 2048 / d;                                                            \
+    const dim3 grid((unsigned)((a.rows.total + rows - 1) / rows * a.n_kv_heads));                                                          \
     hipStream_t st = static_cast<hipStream_t>(stream);                                                                                \
     if (d == 128 && f8) hipLaunchKernelGGL((KERNEL<128, true>), grid, dim3(256), 0, st, a);                                           \
     else if (d == 128) hipLaunchKernelGGL((KERNEL<128, false>), grid, dim3(256), 0, st, a);                                           \

@@ -66,6 +66,7 @@ def test_moves_are_refused(entry):
     assert move(entry, p=params(head_dim=96)) == UNSUPPORTED
     assert move(entry, p=params(batch=0)) == INVALID
     assert move(entry, total=2 ** 28) == UNSUPPORTED
+    assert move(entry, p=params(n_q_heads=1, n_kv_heads=1), total=2 ** 28) == UNSUPPORTED     # more lanes than a launch holds
     assert move(entry, total=0, k=None, v=None) == 0             # nothing to do
 
 
@@ -77,6 +78,7 @@ def test_attention_is_refused():
     assert fwd(p=params(n_q_heads=7)) == INVALID
     assert fwd(p=params(head_dim=32)) == UNSUPPORTED
     assert fwd(total=2 ** 28, splits=1) == UNSUPPORTED
+    assert fwd(p=params(n_q_heads=1, n_kv_heads=1), total=2 ** 24, most=2 ** 24, splits=16, ws_bytes=2 ** 62) == UNSUPPORTED
     assert fwd(p=params(batch=60000, n_kv_heads=200, n_q_heads=200), total=10 ** 6, most=10 ** 6, splits=1024, ws_bytes=2 ** 62) == UNSUPPORTED
     assert fwd(total=0, q=None, o=None, ws=None) == 0
 
