@@ -256,6 +256,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ksa_paged_few_kernel(const 
         const unsigned none = lost;
         const bool whole = none == 0 && sees_all(x);
         if (!whole) {
+            if (F8) ve = (none >> r) & 1 ? 127 : ve;   // (without a page: any exponent)
             bool odd = false;
 #pragma unroll
             for (int i = 0; i < NI; ++i) odd |= take_out_raw<F8>(vr[i]);
@@ -484,7 +485,7 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
         if constexpr (F8) exp_at = spot_exp(a, spot, hkv);
     };
     auto load_v = [&](int i) {
-        if (F8 && i == 0) v_e = next_v_e;
+        if (F8 && i == 0) v_e = lost ? 127 : next_v_e;   // (without a page: any exponent)
         rows[i] = *reinterpret_cast<const u32x4 *>(vb + from[i]);
     };
     auto find_k = [&](int i) { from[i] = lane_value(next_at, i * RPI + f_row) + f_piece * 16; };

@@ -240,6 +240,40 @@ def test_strided_sources_and_outputs():
     assert torch.equal(bits(qkv[:, :2]), bits(rest[:, :2])) and torch.equal(bits(qkv[:, 6:]), bits(rest[:, 6:]))
 
 
+@pytest.mark.parametrize("rows", [1, 3, 40])
+def test_any_number_of_spans(rows):
+    """More spans than keys have blocks, up to the most there may be: the same outputs."""
+    say(f"paged spans rows={rows}")
+    p = K.make_params(2, 4096, 64, 8, 1, 6, 2, 64)
+    for n_splits in (2, 4, 5, 8, 9, 63, 64, 65, 130, 1024):
+        check_attention(p, 16, n_splits % 2 == 0, [2777, 100], [rows, rows], 16, n_splits, rows)
+    p = K.make_params(1, 4096, 64, 8, 1, 3, 1, 128)
+    for n_splits in (4, 8, 9, 100):
+        check_attention(p, 16, False, [2777], [rows], 17, n_splits, rows)
+
+
+def test_calls_without_rows():
+    """No rows at all, and none that belong to a sequence: nothing is touched."""
+    p = K.make_params(2, 1024, 16, 2, 1, 2, 1, 64)
+    pages = Pages(p, [100, 50], 8, False, 5, fill=3.0)
+    none = torch.empty(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    cu, start = batch_of([10, 20], [0, 0])
+    K.ksa_paged_append(pages.cache, none[:, :1], none[:, :1], cu, start)
+    k, v = K.ksa_paged_read(pages.cache, cu, start, 0)
+    o, lse = K.ksa_paged_fwd(pages.cache, none, cu, start)
+    assert k.shape == v.shape == (0, 1, 64) and o.shape == (0, 2, 64) and lse.shape == (0, 2)
+    before = pages.k.clone()
+    for rows in (1, 90):
+        k, v = torch.full((rows, 1, 64), 5.0, device="cuda").to(torch.bfloat16), torch.full((rows, 1, 64), 6.0, device="cuda").to(torch.bfloat16)
+        K.ksa_paged_append(pages.cache, k, v, cu, start)
+        K.ksa_paged_read(pages.cache, cu, start, rows, k=k, v=v)
+        assert bool((k == 5).all()) and bool((v == 6).all()) and torch.equal(pages.k, before)
+        for n_splits in (1, 3, 12):
+            o, lse = torch.full((rows, 2, 64), 5.0, device="cuda").to(torch.bfloat16), torch.full((rows, 2), 6.0, device="cuda")
+            K.ksa_paged_fwd(pages.cache, o, cu, start, o=o, lse=lse, n_splits=n_splits)
+            assert bool((o == 5).all()) and bool((lse == 6).all())
+
+
 # ---- what may not reach a row -------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("fp8", [False, True])
@@ -314,6 +348,35 @@ def test_rows_without_a_page(fp8):
                 want, _, off, _ = attend(q.double(), stands_for(k, fp8), stands_for(v, fp8), list(range(first, first + count)), p)
                 assert bool(torch.isnan(o[sees].float()).all()) and bool(torch.isnan(lse[sees]).all())
                 assert bool(((o.double() - want).abs() <= off)[~sees].all())
+
+
+@pytest.mark.parametrize("rows,n_splits", [(5, 1), (5, 2), (100, 1), (100, 2)])
+def test_exponents_at_the_front_of_the_pool_do_not_reach_rows_by_missing_pages(rows, n_splits):
+    """A missing page's keys, unseen by some of the rows: whatever is read in their place is any number times any power of two."""
+    say(f"paged missing pages, wild exponents rows={rows} splits={n_splits}")
+    p = K.make_params(1, 1024, 16, 2, 1, 2, 1, 64)
+    n = 18 * 20
+    pages = Pages(p, [n], 8, True, 5, fill=448.0)
+    used = torch.cat([pages.text.flatten(), pages.sums.flatten()]).tolist()
+    unused = next(x for x in range(1, pages.k.shape[0]) if x not in used)
+    for host, dev in ((pages.text, pages.text_dev), (pages.sums, pages.sums_dev)):
+        host[host == 0] = unused
+        dev.copy_(host)
+    pages.k_exp.fill_(255), pages.v_exp.fill_(255)
+    k, v = randn(n, 1, 64, seed=6), randn(n, 1, 64, seed=7)
+    pages.put(0, 0, k, v)
+    from tests.paged import kinds, mask
+    _, text, idx = kinds(n, 16, 2)
+    gone = text & (idx // 8 == 33)                       # rows 264 .. 271, the back half of chunk 16
+    pages.text_dev[0, 33] = -1
+    for first in (18 * 16 + 8, 18 * 17 + 14):            # the first rows see them, with the second start the last ones do not
+        count = min(rows, n - first)
+        q = randn(count, 2, 64, seed=9)
+        o, lse = K.ksa_paged_fwd(pages.cache, q, *batch_of([first], [count]), n_splits=n_splits)
+        sees = torch.from_numpy((mask(np.arange(first, first + count), n, 16, 2, 1) & gone).any(1)).cuda()
+        want, want_lse, off, lse_off = attend(q.double(), stands_for(k, True), stands_for(v, True), list(range(first, first + count)), p)
+        assert bool(torch.isnan(o[sees].float()).all()) and bool(torch.isnan(lse[sees]).all())
+        assert bool(((o.double() - want).abs() <= off)[~sees].all()) and bool(((lse.double() - want_lse).abs() <= lse_off)[~sees].all())
 
 
 def test_narrow_tables_are_tables_of_missing_pages():
@@ -542,3 +605,68 @@ def test_a_stream_of_its_own_and_repeated_calls():
         torch.cuda.synchronize()
         for o, lse in outs:
             assert torch.equal(bits(o), bits(o0)) and torch.equal(lse, lse0)
+
+
+@pytest.mark.parametrize("rows", [1, 64])
+def test_what_a_call_allocates_belongs_to_its_stream(rows):
+    """Outputs and workspaces of calls on another stream, whose memory is given back and taken again while they run."""
+    say(f"paged allocations rows={rows}")
+    p = K.make_params(2, 8192, 64, 8, 1, 8, 2, 128)
+    pages = Pages(p, [9000, 8000], 64, False, 5)
+    for b, n in enumerate((9000, 8000)):
+        pages.put(b, 0, randn(n, 2, 128, seed=b), randn(n, 2, 128, seed=b + 5))
+    q = randn(2 * rows, 8, 128, seed=3)
+    cu, start = batch_of([9000 - rows, 8000 - rows], [rows, rows])
+    o0, lse0 = K.ksa_paged_fwd(pages.cache, q, cu, start, max_rows=rows, n_splits=4)
+    k0, v0 = K.ksa_paged_read(pages.cache, cu, start, 2 * rows)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    size = K.paged_workspace_bytes(pages.cache, 2 * rows, rows, 4)
+    for _ in range(8):
+        o, lse = K.ksa_paged_fwd(pages.cache, q, cu, start, max_rows=rows, n_splits=4, stream=side)
+        torch.full((size,), 255, dtype=torch.uint8, device="cuda")        # on the current stream, at once
+        k, v = K.ksa_paged_read(pages.cache, cu, start, 2 * rows, stream=side)
+        torch.full_like(k, 9.0)
+        torch.cuda.synchronize()
+        assert torch.equal(bits(o), bits(o0)) and torch.equal(lse, lse0) and torch.equal(bits(k), bits(k0)) and torch.equal(bits(v), bits(v0))
+
+
+def test_two_graphs_share_a_workspace():
+    say("paged graphs, one workspace")
+    p = K.make_params(2, 4096, 64, 8, 1, 8, 2, 128)
+    pages = Pages(p, [3000, 2000], 64, True, 5)
+    for b, n in enumerate((3000, 2000)):
+        pages.put(b, 0, randn(n, 2, 128, seed=b), randn(n, 2, 128, seed=b + 5))
+    calls, graphs = [], []
+    ws = torch.empty(max(K.paged_workspace_bytes(pages.cache, 2 * rows, rows, 4) for rows in (1, 64)), dtype=torch.uint8, device="cuda")
+    for rows in (1, 64):
+        q = randn(2 * rows, 8, 128, seed=3)
+        cu, start = batch_of([3000 - rows, 2000 - rows], [rows, rows])
+        want = K.ksa_paged_fwd(pages.cache, q, cu, start, max_rows=rows, n_splits=4)
+        got = torch.empty_like(want[0]), torch.empty_like(want[1])
+        calls.append((q, cu, start, want, got))
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            K.ksa_paged_fwd(pages.cache, q, cu, start, max_rows=rows, n_splits=4, workspace=ws, o=got[0], lse=got[1])
+        graphs.append(g)
+    for turn in range(4):
+        for _, _, _, _, got in calls:
+            got[0].zero_(), got[1].zero_()
+        ws.fill_(255)                                      # (NaN)
+        for g in graphs if turn % 2 else graphs[::-1]:
+            g.replay()
+        torch.cuda.synchronize()
+        for _, _, _, want, got in calls:
+            assert torch.equal(bits(want[0]), bits(got[0])) and torch.equal(want[1], got[1])
+
+
+def test_a_cache_keeps_its_own_parameters():
+    p = K.make_params(1, 1024, 16, 2, 1, 2, 1, 64)
+    pages = Pages(p, [100], 8, False, 5)
+    p.batch, p.n_kv_heads = 50, 2
+    k = randn(100, 1, 64, seed=1)
+    cu, start = batch_of([0], [100])
+    K.ksa_paged_append(pages.cache, k, k, cu, start)
+    k2, _ = K.ksa_paged_read(pages.cache, cu, start, 100)
+    assert torch.equal(bits(k2), bits(k))
