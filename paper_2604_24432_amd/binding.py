@@ -541,11 +541,13 @@ class PagedCache:
     """A batch of sequences whose K / V rows lie in the pages of one pool (struct ksa_paged_cache); holds its tensors.
 
     k, v: [n_pages, Hkv, page_rows, d] on the GPU, bfloat16, or float8_e4m3fn with k_exp, v_exp uint8 [n_pages, Hkv, page_rows].
-    text_table, summary_table: int32 [batch, columns], contiguous; their contents may change from call to call.
+    text_table, summary_table: int32 [batch, columns], contiguous; their contents may change from call to call.  Other tensors, or other
+    parameters, take another PagedCache.
     """
 
     def __init__(self, params: ksa_params, k, v, text_table, summary_table=None, k_exp=None, v_exp=None):
         import torch
+        params = ksa_params.from_buffer_copy(params)
         f8 = k.dtype is torch.float8_e4m3fn
         for t, name in ((k, "k"), (v, "v")):
             _require(t, name, torch.float8_e4m3fn if f8 else torch.bfloat16, 4)
@@ -631,15 +633,19 @@ def _rows_of_call(cache: PagedCache, tensors, heads, cu_rows, start):
         raise ValueError("tensors lie on another device than the cache")
 
 
+def _check_stream(cache: PagedCache, stream):
+    if stream.device != cache.device:
+        raise ValueError("stream belongs to another device than the cache")
+
+
 def _paged(cache: PagedCache, name, stream, *args):
     """The call, on the cache's device: on `stream`, or on that device's current one."""
     from torch import _C
     here, there = _C._cuda_getDevice(), cache._dev
     if stream is None:
         raw = _C._cuda_getCurrentRawStream(there)
-    elif stream.device != cache.device:
-        raise ValueError("stream belongs to another device than the cache")
     else:
+        _check_stream(cache, stream)
         raw = stream.cuda_stream
     if here == there:
         rc = getattr(lib(), name)(*cache._args, *args, raw)
@@ -666,8 +672,13 @@ def ksa_paged_append(cache: PagedCache, k_new, v_new, cu_rows, start, stream=Non
 
 
 def ksa_paged_read(cache: PagedCache, cu_rows, start, total_rows: int, k=None, v=None, stream=None):
-    """The rows that ksa_paged_append with these cu_rows and start would write -> k, v [total_rows, Hkv, d] bf16."""
+    """The rows that ksa_paged_append with these cu_rows and start would write -> k, v [total_rows, Hkv, d] bf16.
+    What is allocated here belongs to `stream`."""
     import torch
+    if stream is not None and (k is None or v is None):
+        _check_stream(cache, stream)
+        with torch.cuda.stream(stream):
+            return ksa_paged_read(cache, cu_rows, start, total_rows, k, v)
     if k is None:
         k = torch.empty((total_rows, *cache._kv), dtype=torch.bfloat16, device=cache.device)
     if v is None:
@@ -688,8 +699,12 @@ def ksa_paged_fwd(cache: PagedCache, q, cu_rows, start, max_rows: Optional[int] 
                   n_splits: int = 0, stream=None):
     """q [rows, Hq, d] bf16, the queries of the rows that ksa_paged_append wrote -> o like q, lse [rows, Hq] fp32.
     max_rows: the largest number of rows of a sequence (all of them if omitted); workspace: uint8, at least
-    paged_workspace_bytes(cache, rows, max_rows, n_splits) bytes (allocated here if omitted)."""
+    paged_workspace_bytes(cache, rows, max_rows, n_splits) bytes (allocated here if omitted).  What is allocated here belongs to `stream`."""
     import torch
+    if stream is not None and (o is None or workspace is None or lse is None and return_lse):
+        _check_stream(cache, stream)
+        with torch.cuda.stream(stream):
+            return ksa_paged_fwd(cache, q, cu_rows, start, max_rows, o, lse, return_lse, workspace, n_splits)
     rows = q.shape[0]
     if max_rows is None:
         max_rows = max(rows, 1)
