@@ -147,6 +147,20 @@ __device__ __forceinline__ float raised(const f32x16 &sc, float sum, float m_run
         for (int g = 0; g < 16; ++g) o[db][g] *= alpha;
     return m;
 }
+// The scores of 32 keys where not all are seen by all: a lane's are those of keys 8 (g / 4) + 4 h + g % 4.  Bit i of `sees`: the row sees key i, of `none`:
+// it has no page.  (Two vector instructions per score, from bits spread over words; comparing positions took twelve: 3.0 us per tile of
+// 64 keys and 128 pairs against 1.3 where all is seen.)
+__device__ __forceinline__ void hide(f32x16 &sc, unsigned sees, unsigned none, int h) {
+    const unsigned see = sees >> (4 * h), gone = none >> (4 * h);
+    auto spread = [](unsigned x, int g) { return (unsigned)((int)(x << (31 - 8 * (g / 4) - g % 4)) >> 31); };   // all bits of a word
+    auto choose = [](unsigned which, unsigned x, unsigned y) { return (which & x) | (~which & y); };
+    if (none != 0) {
+#pragma unroll
+        for (int g = 0; g < 16; ++g) sc[g] = __builtin_bit_cast(float, choose(spread(gone, g), 0x7fc00000u, __builtin_bit_cast(unsigned, (float)sc[g])));
+    }
+#pragma unroll
+    for (int g = 0; g < 16; ++g) sc[g] = __builtin_bit_cast(float, choose(spread(see, g), __builtin_bit_cast(unsigned, (float)sc[g]), 0xff800000u));
+}
 // The elements of a V row that are no numbers, to the output of a row that sees it.
 template <int D, bool F8>
 __device__ __forceinline__ void add_no_numbers(const FwdArgs &a, int hkv, const Spot &at, int h, bool see, f32x16 (&o)[D / 32]) {
@@ -273,14 +287,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ksa_paged_few_kernel(const 
         for (int g = 0; g < 16; ++g) sc[g] = 0.f;
 #pragma unroll
         for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(k_at + s * 32), q[s], sc, 0, 0, 0);
-        if (!whole) {
-#pragma unroll
-            for (int g = 0; g < 16; ++g) {
-                const int key = 8 * (g / 4) + 4 * h + g % 4;
-                const float lost_or_not = (none >> key) & 1 ? __builtin_nanf("") : sc[g];
-                sc[g] = seen.sees(x + key) ? lost_or_not : -INFINITY;
-            }
-        }
+        if (!whole) hide(sc, seen.sees_32(x), none, h);
         bf16x8 p[2];
         float sum = 0.f;
         auto weights = [&]() {
@@ -467,35 +474,34 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
 #pragma unroll
     for (int s = 0; s < KS; ++s) q[s] = scaled_q(a.q + q_row * a.q_row + q_head * a.q_head + s * 16 + h * 8, a.q_scale);
 
-    // ---- tiles on their way: table entries two tiles ahead, rows into registers one ahead, then as bf16 into LDS; V a step behind K --
+    // ---- tiles on their way: table entries three tiles ahead, rows into registers, then as bf16 into LDS; V a step behind K.  A row is asked for a
+    // whole step before it goes to LDS: with one workgroup on a compute unit nothing else hides how long it takes. --------------------
     const unsigned char *const kb = a.k + hkv * a.head_bytes, *const vb = a.v + hkv * a.head_bytes;
     const int f_row = lane / LPR % RPI, f_piece = lane % LPR;   // (lanes beyond the rows repeat them)
     Entry entry;                               // of row RW * wave + lane % RW of a tile
     int64_t next_at = 0;                       // where that row of the next K tile lies
     int64_t exp_at = 0;                        // ... and its exponents
-    int k_e = 0, v_e = 0, next_v_e = 0;
-    int64_t from[NI];                          // where the rows of the lane's loads lie: the V tile's, then the K tile's
-    u32x4 rows[NI];                            // ... of V in half 0, of K in half 1
+    int k_e = 0, v_e = 0, next_k_e = 0, next_v_e = 0;
+    int64_t from[NI];                          // where the rows of the lane's loads lie: of the K tile asked for last, then of the V tile
+    u32x4 k_rows[NI], v_rows[NI];
     bool lost = false, next_lost = false, odd = false;   // row lane % RW of the K tile on its way has no page; elements of V were taken out
-    auto look = [&](int t) { entry = entry_of(a.rows, tile.b, key_at(keys, min(t * BN + RW * wave + lane % RW, keys.n - 1))); };
+    const int last = min(keys.n, end_tile * BN) - 1;
+    auto look = [&](int t) { entry = entry_of(a.rows, tile.b, key_at(keys, min(t * BN + RW * wave + lane % RW, last))); };
     auto settle = [&]() {
         const Spot spot = spot_of(a.rows, entry);
         next_lost = spot.page < 0;
         next_at = spot_bytes(a, spot);
         if constexpr (F8) exp_at = spot_exp(a, spot, hkv);
     };
-    auto load_v = [&](int i) {
-        if (F8 && i == 0) v_e = lost ? 127 : next_v_e;   // (without a page: any exponent)
-        rows[i] = *reinterpret_cast<const u32x4 *>(vb + from[i]);
+    auto find = [&](int i) { from[i] = lane_value(next_at, i * RPI + f_row) + f_piece * 16; };
+    auto load_exps = [&]() {
+        if constexpr (F8) next_k_e = a.k_exp[exp_at], next_v_e = a.v_exp[exp_at];
     };
-    auto find_k = [&](int i) { from[i] = lane_value(next_at, i * RPI + f_row) + f_piece * 16; };
-    auto load_k = [&](int i) {
-        if (i == 0) {
-            lost = next_lost;
-            if constexpr (F8) k_e = a.k_exp[exp_at], next_v_e = a.v_exp[exp_at];
-        }
-        rows[i] = *reinterpret_cast<const u32x4 *>(kb + from[i]);
+    auto take_exps = [&]() {   // (a step after they were asked for)
+        if constexpr (F8) k_e = next_k_e, v_e = lost ? 127 : next_v_e;   // (without a page: any exponent)
     };
+    auto load_k = [&](int i) { k_rows[i] = *reinterpret_cast<const u32x4 *>(kb + from[i]); };
+    auto load_v = [&](int i) { v_rows[i] = *reinterpret_cast<const u32x4 *>(vb + from[i]); };
     auto put = [&](const u32x4 &x, int e, int i, unsigned char *to) {
         u32x4 y[F8 ? 2 : 1];
         as_bf16<F8>(x, F8 ? power_of_two(__shfl(e, i * RPI + f_row)) : 1.f, y);
@@ -503,8 +509,8 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
         for (int z = 0; z < (F8 ? 2 : 1); ++z) *reinterpret_cast<u32x4 *>(to + z * 16) = y[z];
     };
     const int put_k_at = (RW * wave + f_row) * KROW + f_piece * (F8 ? 32 : 16), put_v_at = 2 * K_BYTES + (RW * wave + f_row) * VROW + f_piece * (F8 ? 32 : 16);
-    auto put_k = [&](int t, int i) { put(rows[i], k_e, i, lds + (t & 1) * K_BYTES + put_k_at + i * RPI * KROW); };
-    auto put_v = [&](int t, int i) { put(rows[i], v_e, i, lds + (t & 1) * V_BYTES + put_v_at + i * RPI * VROW); };
+    auto put_k = [&](int t, int i) { put(k_rows[i], k_e, i, lds + (t & 1) * K_BYTES + put_k_at + i * RPI * KROW); };
+    auto put_v = [&](int t, int i) { put(v_rows[i], v_e, i, lds + (t & 1) * V_BYTES + put_v_at + i * RPI * VROW); };
     auto put_state = [&](int t) {   // with K tile t and V tile t - 1
         const unsigned none = (unsigned)__builtin_amdgcn_ballot_w64(lost) & ((1u << RW) - 1), taken = __builtin_amdgcn_ballot_w64(odd) != 0 ? 1u << 31 : 0u;
         if (lane == 0) sh_state[t & 1][wave] = none | taken;
@@ -627,12 +633,7 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
                 unsigned none = 0;   // keys without a page
 #pragma unroll
                 for (int x = 0; x < NW / 2; ++x) none |= (sh_state[t & 1][y * (NW / 2) + x] & ((1u << RW) - 1)) << (x * RW);
-#pragma unroll
-                for (int g = 0; g < 16; ++g) {
-                    const int key = 8 * (g / 4) + 4 * h + g % 4;
-                    const float lost_or_not = (none >> key) & 1 ? __builtin_nanf("") : sc[y][g];
-                    sc[y][g] = seen.sees(x0 + key) ? lost_or_not : -INFINITY;
-                }
+                hide(sc[y], seen.sees_32(x0), none, h);
             }
         }
     };
@@ -640,32 +641,32 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
     using No = std::false_type;
     const std::integral_constant<int, 0> y0;
     const std::integral_constant<int, 1> y1;
-    // Slots of a half: KS, and as many again.  Half 0 brings V of this tile to LDS, half 1 K of the next; where the rows of the one after that
-    // are, is worked out on the way.
+    // Slots of a half: KS, and as many again.  Half 0 brings V of this tile to LDS and asks for the next, half 1 K of the next tile and asks
+    // for the one after that; where its rows are, is worked out on the way.
     auto bring_v = [&](int t) {
         return [&, t](int x) {
-            if (x < NI) load_v(x);
-            if (x >= NI && x < 2 * NI) find_k(x - NI);
             if (x == 2 * KS - NI) {
                 odd = false;
                 if (!tile_all.sees_all(t * BN, t * BN + BN)) {
 #pragma unroll
-                    for (int i = 0; i < NI; ++i) odd |= take_out_raw<F8>(rows[i]);
+                    for (int i = 0; i < NI; ++i) odd |= take_out_raw<F8>(v_rows[i]);
                 }
             }
-            if (x >= 2 * KS - NI) put_v(t, x - (2 * KS - NI));
+            if (x >= 2 * KS - NI) put_v(t, x - (2 * KS - NI)), load_v(x - (2 * KS - NI));
         };
     };
     auto bring_k = [&](int t) {
         return [&, t](int x) {
-            if (x < NI) load_k(x);
-            if (x == NI) settle();
-            if (x == NI + 1) look(t + 2);
-            if (x == 2 * KS - NI) put_state(t);
-            if (x >= 2 * KS - NI) put_k(t, x - (2 * KS - NI));
+            if (x == 0) take_exps();
+            if (x == 1) settle();
+            if (x == 2) look(t + 2);
+            if (x == 3) load_exps();
+            if (x >= 4 && x < 4 + NI) find(x - 4);
+            if (x == 2 * KS - NI) put_state(t), lost = next_lost;
+            if (x >= 2 * KS - NI) put_k(t, x - (2 * KS - NI)), load_k(x - (2 * KS - NI));
         };
     };
-    static_assert(3 * NI <= 2 * KS, "in one half");
+    static_assert(4 + 2 * NI <= 2 * KS, "in one half");
     auto nothing = [](int) {};
     auto begin = [&](int t) {
         __syncthreads();
@@ -682,14 +683,23 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
     if (first_tile < end_tile) {
         look(first_tile);
         settle();
-#pragma unroll
-        for (int i = 0; i < NI; ++i) find_k(i), load_k(i);
+        lost = next_lost;
         look(first_tile + 1);
+        load_exps();
+#pragma unroll
+        for (int i = 0; i < NI; ++i) find(i), load_k(i);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) load_v(i);
+        take_exps();
 #pragma unroll
         for (int i = 0; i < NI; ++i) put_k(first_tile, i);
         put_state(first_tile);
         settle();
+        lost = next_lost;
         look(first_tile + 2);
+        load_exps();
+#pragma unroll
+        for (int i = 0; i < NI; ++i) find(i), load_k(i);
         begin(first_tile);
         half(first_tile, y0, Yes{}, No{}, No{}, bring_v(first_tile));
         half(first_tile, y1, Yes{}, Yes{}, No{}, bring_k(first_tile + 1));

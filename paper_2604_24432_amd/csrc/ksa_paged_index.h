@@ -114,6 +114,10 @@ struct Seen {
     int a, b, c, d;
     // (no && and ||: they would become branches)
     KSA_INDEX bool sees(int x) const { return ((x >= a) & (x < b)) | ((x >= c) & (x < d)); }
+    KSA_INDEX unsigned sees_32(int x) const {   // bit i: key x + i
+        return (upto(b - x) & ~upto(a - x)) | (upto(d - x) & ~upto(c - x));
+    }
+    KSA_INDEX static unsigned upto(int n) { return n >= 32 ? ~0u : (1u << max(n, 0)) - 1; }   // the first n bits
     KSA_INDEX bool sees_all(int x, int end) const { return ((x >= a) & (end <= b)) | ((x >= c) & (end <= d)); }
     KSA_INDEX bool sees_any(int x, int end) const { return (max(x, a) < min(end, b)) | (max(x, c) < min(end, d)); }
 };

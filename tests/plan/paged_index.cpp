@@ -58,6 +58,9 @@ static void check_list(const PagedRows &a, const Keys &k, const std::vector<int>
             if (s.sees_all(x, x + 8) && !all) fail("not all are seen", q, x);
             if (s.sees_any(x, x + 8) != any) fail("any seen", q, x);
         }
+        for (int x = -40; x < k.n + 40; x += 13)
+            for (int i = 0; i < 32; ++i)
+                if (((s.sees_32(x) >> i) & 1) != (s.sees(x + i) ? 1u : 0u)) fail("32 keys together", q, x);
         if (s.sees(-1) || s.sees(k.n)) fail("positions outside the list", q, k.n);
     }
     (void)every;
