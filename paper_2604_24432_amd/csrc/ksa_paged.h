@@ -30,6 +30,7 @@ struct KsaPagedPlan {
     bool few;                     // the kernel for few rows: at most KSA_PAGED_FEW (row, query head) pairs of a sequence and KV head
     int32_t n_splits;             // spans of the keys
     int32_t pairs;                // many rows: (row, query head) pairs of a query tile, 128 or 256
+    int32_t groups;               // ... of 128: groups of waves with a part of the keys each, 1 or 2
     int32_t slots;                // ... and query tiles of all sequences, none less
 };
 // Floats of a span's record for one (row, query head): the output, then maximum and sum (padded to 16 bytes)

@@ -1,9 +1,11 @@
 // Attention of new rows over the paged cache for gfx950.
 //
-// Two kernels.  Few (row, query head) pairs of a KV head (ksa_paged_few_kernel): every wave streams blocks of 32 keys of its own, K from HBM
-// into the registers of the score product's operand, V through LDS, once for all pairs.  Many (ksa_paged_many_kernel): a workgroup holds 128
-// pairs, 32 per wave, and walks tiles of 64 keys that its waves share in LDS.  Either may cut the keys into spans, one workgroup each,
-// whose records a third kernel joins by log-sum-exp.
+// o = sum_x w_x v_x / sum_x w_x, w_x = 2^(s_x - m) over the keys x that a row sees, s = log2(e) scale q k, m a reference of the row's.  Two kernels, each one
+// pass over the keys, both products on the matrix unit with the keys as rows of the first and the (row, query head) pairs as its columns, so that a
+// lane has its pair's weights where the second product wants them.  Few pairs of a KV head (ksa_paged_few_kernel): bound by the cache's bytes, so every wave
+// streams blocks of 32 keys of its own, once for all pairs.  Many (ksa_paged_many_kernel): bound by the products, so a workgroup holds 128 or 256
+// pairs, 32 per wave, and walks tiles of 64 keys that its waves share in LDS.  Either may cut the keys into spans, one workgroup each, whose
+// records a third kernel joins by log-sum-exp.
 //
 // The keys that a group of rows sees together form one list, summaries first, then text (Eq. 3); where a position of the list lies is
 // looked up in the tables a block ahead of its loads.  8-bit rows become bf16 on their way to the operands, exactly: the conversion takes the power
@@ -120,9 +122,12 @@ __device__ __forceinline__ bf16x8 scaled_q(const __bf16 *q, float by) {
 
 __device__ __forceinline__ float log_sum(float m, float l) { return (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f; }
 
-// A row's weights go by a reference that is one of its scores, not the largest: no weight is too small to count, and the sum of 16 of them is
-// looked at instead of their scores.  Above this a new reference is taken and the 16 are worked out again.
-constexpr float HIGH = 1048576.f;
+// Many rows: a row's reference is one of its scores, not always the largest: no weight is too small to count, and the sum of 16 of them is looked
+// at instead of their scores.  Above this the largest becomes the reference and the 16 are worked out again.  In range 2^20 would do, but a weight of 1
+// is exact in bf16 and the largest one's rounding is what the output keeps of all of them: off by 1.40 times an output's own rounding (4000 keys,
+// half of the scores within 1), with 128 1.22, with 64 1.12.  Time: full attention of 2048 rows over 64K keys 1997 us with 2^20, 2029 with 128, 2067 with 64;
+// window of 1023 30.2, 32.0, 33.2; a running maximum takes eight more vector instructions of a hundred in every half, 64 more where it moves.
+constexpr float HIGH = 128.f;
 
 // Bytes from one row of a tile to the next in LDS: the 16 rows of a phase of the plain reads of K, 16 bytes each, and the 4 rows of one of the
 // transposing reads of V, 64 bytes each, lie in different banks, and every address is a base plus a constant.
@@ -298,11 +303,19 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ksa_paged_few_kernel(const 
                 sum += w, p[g / 8][g % 8] = (__bf16)w;
             }
         };
-        weights();
-        if (__builtin_amdgcn_ballot_w64(sum > HIGH) != 0) {
-            m_run = raised(sc, sum, m_run, a.score_scale, l_run, o);
-            weights();
+        float most = sc[0];
+#pragma unroll
+        for (int g = 1; g < 16; ++g) most = fmaxf(most, sc[g]);
+        most = fmaxf(most, swap32(most)) * a.score_scale;
+        if (__builtin_amdgcn_ballot_w64(most > m_run) != 0) {
+            const float m = fmaxf(most, m_run), alpha = __builtin_amdgcn_exp2f(m_run - m);
+            m_run = m, l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int g = 0; g < 16; ++g) o[db][g] *= alpha;
         }
+        weights();
         l_run += sum;
 #pragma unroll
         for (int y = 0; y < 2 * DB; ++y) {   // 16 keys y / DB, columns 32 (y % DB) ..
@@ -418,21 +431,24 @@ __device__ __forceinline__ Tile tile_of(const FwdArgs &a, int slot) {
 
 // A step works on one tile of keys in two halves of 32.  What a half does: the scores of its keys, the weights of the half before, and the
 // product with V of the half before that, so that the matrix unit's and the vector unit's work do not wait for each other.
-// NW waves, 32 pairs each.
-template <int D, bool F8, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArgs a) {
+// GROUPS groups of NW waves, 32 pairs each.  Two groups have the same pairs, each half of the keys, and their results are put together in LDS.
+template <int D, bool F8, int NW, int GROUPS>
+__global__ __launch_bounds__(NW * GROUPS * 64, 2) void ksa_paged_many_kernel(const FwdArgs a) {
     constexpr int KS = D / 16, DB = D / 32, ES = F8 ? 1 : 2, PAIRS = NW * 32;
     constexpr int RW = BN / NW;                                       // rows of a tile that a wave fetches
     constexpr int LPR = D * ES / 16, RPI = 64 / LPR < RW ? 64 / LPR : RW, NI = RW / RPI;   // lanes per row, rows per load, loads per wave and tensor
     constexpr int KROW = TileRow<D>::K, VROW = TileRow<D>::V, K_BYTES = BN * KROW, V_BYTES = BN * VROW;
     constexpr int STAGE_ROW = D * 2 + 16;
     static_assert(RW % RPI == 0 && NI >= 1, "a wave's rows are whole loads");
-    static_assert(NW * 32 * STAGE_ROW <= 2 * (K_BYTES + V_BYTES), "the results pass through the tiles' memory");
-    __shared__ __align__(16) unsigned char lds[2 * (K_BYTES + V_BYTES)];   // two buffers of K, two of V
-    __shared__ __align__(16) unsigned sh_state[2][NW];   // of the K tile: which of a wave's rows have no page; bit 31: of the V tile before: elements were taken out
+    constexpr int OWN = 2 * (K_BYTES + V_BYTES);   // of a group: two buffers of K, two of V
+    static_assert(NW * 32 * STAGE_ROW <= OWN && (GROUPS == 1 || NW * 64 * (16 * DB + 2) * 4 <= OWN), "the results pass through the tiles' memory");
+    __shared__ __align__(16) unsigned char sh_tiles[GROUPS * OWN];
+    __shared__ __align__(16) unsigned sh_states[GROUPS][2][NW];   // of the K tile: which of a wave's rows have no page; bit 31: of the V tile before: elements were taken out
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6) % NW, group = __builtin_amdgcn_readfirstlane(tid >> 6) / NW;
     const int r = lane & 31, h = lane >> 5;
+    unsigned char *const lds = sh_tiles + group * OWN;
+    unsigned (*const sh_state)[NW] = sh_states[group];
     // KV heads fastest: with a multiple of 8 of them the tiles of one share an L2
     const int rest = ksa_div(blockIdx.x, a.by_heads), hkv = blockIdx.x - rest * a.n_kv_heads;
     const int slot = ksa_div(rest, a.by_splits), split = rest - slot * a.n_splits;
@@ -443,7 +459,7 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
     const int n_pairs = (int)min((int64_t)PAIRS, (int64_t)n_rows * a.group - tile.first);
     if (!seq.ok) {
         if (a.n_splits > 1) return;   // (the joining kernel sees to it)
-        for (int x = tid; x < n_pairs * D; x += NW * 64) {
+        for (int x = tid; x < n_pairs * D; x += NW * GROUPS * 64) {
             const int pair = tile.first + x / D, row = pair / a.group, hq = hkv * a.group + pair % a.group;
             a.o[(seq.first + row) * a.o_row + hq * a.o_head + x % D] = (__bf16)__builtin_nanf("");
             if (a.lse && x % D == 0) a.lse[(int64_t)(seq.first + row) * a.n_q_heads + hq] = __builtin_nanf("");
@@ -459,7 +475,8 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
     auto all_of = [&](const Visible &first, const Visible &last) { return seen_of(keys, Visible{last.lo_s, first.hi_s, last.lo_t, first.hi_t}); };
     const Seen tile_all = all_of(v_lo, v_hi), wave_all = all_of(visible(a.rows, row_at(wave * 32)), visible(a.rows, row_at(wave * 32 + 31)));
     const int n_tiles = (keys.n + BN - 1) / BN, per = ksa_div(n_tiles + a.n_splits - 1, a.by_splits);
-    const int first_tile = split * per, end_tile = min(n_tiles, first_tile + per);
+    const int span = split * per, span_end = min(n_tiles, span + per), steps = max(span_end - span + GROUPS - 1, 0) / GROUPS;   // steps of any group
+    const int first_tile = span + group * steps, end_tile = min(span_end, first_tile + steps);
 
     // packed row and query head of a pair
     auto place_of = [&](int pair, int &row, int &hq) {
@@ -712,6 +729,10 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
         half(end_tile, y0, No{}, Yes{}, Yes{}, nothing);
         half(end_tile, y1, No{}, No{}, Yes{}, nothing);
     }
+    if constexpr (GROUPS > 1) {   // as many barriers in every group
+        for (int t = max(end_tile - first_tile, 0); t < steps; ++t) __syncthreads();
+        if (end_tile <= first_tile && steps > 0) __syncthreads();
+    }
 
     // ---- results ---------------------------------------------------------------------------------------------------------
     if (ever >> 31) {   // what was taken out of V, to the rows that see it
@@ -721,7 +742,22 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
             add_no_numbers<D, F8>(a, hkv, spot_of(a.rows, entry_of(a.rows, tile.b, key_at(keys, x))), h, seen.sees(x), o);
         }
     }
-    const float l = l_run + swap32(l_run);
+    float l = l_run + swap32(l_run);
+    if constexpr (GROUPS > 1) {
+        float *const other = reinterpret_cast<float *>(sh_tiles + OWN) + wave * 64 * (16 * DB + 2) + lane;   // of the lane with the same pair
+        __syncthreads();
+        if (group == 1) {
+#pragma unroll
+            for (int x = 0; x < 16 * DB; ++x) other[x * 64] = o[x / 16][x % 16];
+            other[16 * DB * 64] = m_run, other[(16 * DB + 1) * 64] = l;
+        }
+        __syncthreads();
+        if (group == 1) return;
+        const float m = other[16 * DB * 64], M = fmaxf(m_run, m), w = __builtin_amdgcn_exp2f(m_run - M), v = __builtin_amdgcn_exp2f(m - M);
+#pragma unroll
+        for (int x = 0; x < 16 * DB; ++x) o[x / 16][x % 16] = o[x / 16][x % 16] * w + other[x * 64] * v;
+        l = l * w + other[(16 * DB + 1) * 64] * v, m_run = M;
+    }
     const bool mine = wave * 32 + r < n_pairs;
     if (a.n_splits > 1) {
         if (!mine) return;
@@ -736,7 +772,7 @@ __global__ __launch_bounds__(NW * 64, 2) void ksa_paged_many_kernel(const FwdArg
     }
     if (a.lse && h == 0 && mine) a.lse[(int64_t)q_row * a.n_q_heads + q_head] = log_sum(m_run, l);
     // whole rows are stored: through memory of the wave's own, where the tiles were
-    __syncthreads();
+    if constexpr (GROUPS == 1) __syncthreads();
     unsigned char *const stage = lds + wave * 32 * STAGE_ROW;
     const float inv = 1.f / l;
 #pragma unroll
@@ -864,8 +900,9 @@ void launch(const FwdArgs &a, const KsaPagedPlan &plan, hipStream_t st) {
     if (plan.few) hipLaunchKernelGGL((ksa_paged_few_kernel<D, F8>), few, dim3(FEW_WAVES * 64), 0, st, a);
     else {
         const dim3 many((unsigned)(plan.slots * plan.n_splits * a.n_kv_heads));
-        if (plan.pairs == 128) hipLaunchKernelGGL((ksa_paged_many_kernel<D, F8, 4>), many, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((ksa_paged_many_kernel<D, F8, 8>), many, dim3(512), 0, st, a);
+        if (plan.groups == 2) hipLaunchKernelGGL((ksa_paged_many_kernel<D, F8, 4, 2>), many, dim3(512), 0, st, a);
+        else if (plan.pairs == 128) hipLaunchKernelGGL((ksa_paged_many_kernel<D, F8, 4, 1>), many, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((ksa_paged_many_kernel<D, F8, 8, 1>), many, dim3(512), 0, st, a);
     }
     if (plan.n_splits == 1) return;
     const int items = a.rows.total * a.n_q_heads;

@@ -76,19 +76,19 @@ int64_t most_keys(const ksa_params *p, int64_t rows) {
  * 1 13.6, 3 15.0; 256, 1500, 4 rows, 8-bit 1 26.2, 2 27.0; 256, 4000 1 57.6, 2 57.2, 4 55.9; 512, 16500 1 636, 2 641, 4 656; 16, 65536, 8 rows 8 99, 16 89,
  * 32 91.  Spans dealt by the sequences' lengths (lengths 1 : 4): 128 57.4, the same number each 53.8; 512 248, 249.
  *
- * Many rows: tiles of 128 pairs, two on a compute unit, or of 256, which take their keys from memory half as often but fill a unit alone.  Tiles
- * and spans are chosen by what they are expected to take: a start and an end, the key tiles of a span one after the other, rounds where there are
- * more workgroups than places, and for the records of several spans a second kernel.  Per key tile of head_dim 128: 128 pairs 1.75 alone on a unit,
- * 2.05 in pairs, 256 pairs 1.85.  Measured, tiles x spans: full attention, 2048 rows, 64K keys, 32/8 heads 256 x 1 2020, 128 x 1 2194; 512
- * rows 256 x 4 534, 128 x 4 584, 256 x 3 615, 256 x 8 572; summaries, 512 rows, 4700 keys 256 x 4 52, 128 x 4 55, 128 x 2 62, 256 x 1 119; 2304 rows,
- * 2000 keys 128 x 1 61, 256 x 1 75, 128 x 2 88; 2048 rows, 10000 keys 256 x 1 265, 128 x 1 276, 256 x 2 284; 8 x 100 rows, 4200 keys 128 x 4 52, 128 x 3 59,
- * 256 x 3 61, 128 x 1 110; window of 1023, 1280 rows, 16/16 heads 128 x 3 37, 128 x 1 39, 128 x 4 46, 256 x 3 40; 2595 rows of six sequences, 2700 keys, 12/4
- * heads, head_dim 64 128 x 2 41, 128 x 4 48, 128 x 1 56, 256 x 3 50; 64 rows, 830 keys, 8/4 heads 128 x 6 12.7, 128 x 1 20, 256 x 6 13.9.  Over twelve such
- * calls what is chosen takes 0.6 % longer than the best of 1, 2, 3, 4, 6 and 8 spans.
+ * Many rows: tiles of 128 pairs, two on a compute unit; of 128, alone, whose two groups of waves have half of the keys each; of 256, alone, which take
+ * their keys from memory half as often.  The kind and the spans are chosen by what they are expected to take: a start and an end, the key tiles of
+ * a span one after the other, rounds where there are more workgroups than places, and for the records of several spans a second kernel.  Per key
+ * tile of head_dim 128: 128 pairs 1.5 alone on a unit, 1.95 in pairs, two groups 1.0, 256 pairs 1.75.  Measured, spans each (128 | two groups | 256):
+ * full attention, 2048 rows, 64K keys, 32/8 heads 1 2160 | - | 1990; 512 rows 4 575, 8 608 | 2 562, 4 589 | 3 584, 4 520, 8 557; summaries, 512 rows, 4700
+ * keys 1 94, 4 55 | 1 71, 2 52 | 3 57, 4 52; 2304 rows, 2000 keys 1 56, 2 82 | 1 71 | 1 67; 2048 rows, 10000 keys 1 281 | 1 290 | 1 258, 2 278; 8 x 100 rows, 4200
+ * keys 1 91, 4 46, 6 49 | 1 69, 2 46 | 3 55; window of 1023, 1280 rows, 16/16 heads 1 37, 3 35 | 1 32, 2 49 | 3 37; 2595 rows of six sequences, 2700 keys, 12/4
+ * heads, head_dim 64 1 49, 2 39 | 1 39 | 3 46; 64 rows, 830 keys, 8/4 heads 1 20, 6 12.3 | 6 13.3 | 6 13.4.  Over twelve such calls what is chosen takes 1 %
+ * longer than the best of the three kinds with 1, 2, 3, 4, 6, 8 and 12 spans; without the second kind 3 %.
  */
 KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_rows, int32_t n_splits) {
     const int32_t group = p->n_q_heads / p->n_kv_heads;
-    KsaPagedPlan plan = {false, n_splits, 0, 0};
+    KsaPagedPlan plan = {false, n_splits, 0, 0, 0};
     if (max_rows * group <= KSA_PAGED_FEW) {
         plan.few = true;
         const int64_t units = (int64_t)p->batch * p->n_kv_heads;
@@ -99,21 +99,27 @@ KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_row
         return plan;
     }
     const double size = p->head_dim == 128 ? 1.0 : 0.7;
-    const double records = 1.5e-6 * (double)total_rows * p->n_q_heads * ksa_paged_record(p->head_dim);   // written and read, of one span
+    const double records = 1.35e-6 * (double)total_rows * p->n_q_heads * ksa_paged_record(p->head_dim);   // written and read, of one span
     double best = 0;
-    for (const int32_t pairs : {128, 256}) {
+    struct Kind {
+        int32_t pairs, groups;
+        double start, tile;   // a workgroup's start and end, a tile of keys
+    };
+    for (const Kind &kind : {Kind{128, 1, 3, 1.5}, Kind{128, 2, 6.5, 1.0}, Kind{256, 1, 6, 1.75}}) {
         // every sequence ends one tile of text and one of summaries before it is full; the latter's lists are short
+        const int32_t pairs = kind.pairs;
         const int64_t slots = total_rows * group / pairs + (p->n_summary > 0 ? 2 : 1) * (int64_t)p->batch;
         const double rows = (double)total_rows * p->chunk_len / (p->chunk_len + p->n_summary);
         const double full = rows * group / pairs, units = (p->batch == 1 ? std::ceil(full) : full + 0.5 * p->batch) * p->n_kv_heads;
         const int64_t tiles = (most_keys(p, std::min<int64_t>(max_rows, pairs / group + 1)) + 63) / 64;
         for (int32_t n = n_splits == 0 ? 1 : n_splits; n <= (n_splits == 0 ? 64 : n_splits); ++n) {
             if (n_splits == 0 && n > 1 && n > tiles) break;
-            const double places = pairs == 128 ? 512 : 256, wgs = units * n;
-            const double tile = size * (pairs == 256 ? 1.85 : 1.75 + 0.3 * std::min(std::max((wgs - 256) / 256, 0.0), 1.0));
-            const double rounds = std::max(1.0, 1.03 * wgs / places);   // (workgroups of different lengths)
-            const double time = rounds * ((pairs == 256 ? 6.5 : 4) + (double)((tiles + n - 1) / n) * tile) + (n > 1 ? 3.5 + records * n : 0);
-            if (plan.slots == 0 || time < best) best = time, plan.pairs = pairs, plan.slots = (int32_t)slots, plan.n_splits = n;
+            const bool two = pairs == 128 && kind.groups == 1;   // on a compute unit
+            const double places = two ? 512 : 256, wgs = units * n;
+            const double tile = size * (kind.tile + (two ? 0.45 * std::min(std::max((wgs - 256) / 256, 0.0), 1.0) : 0));
+            const double rounds = std::max(1.0, 1.1 * wgs / places);   // (workgroups of different lengths)
+            const double time = rounds * (kind.start + (double)((tiles + n - 1) / n) * tile) + (n > 1 ? 5 + records * n : 0);
+            if (plan.slots == 0 || time < best) best = time, plan.pairs = pairs, plan.groups = kind.groups, plan.slots = (int32_t)slots, plan.n_splits = n;
         }
     }
     return plan;
@@ -125,7 +131,7 @@ constexpr int64_t MOST_LANES = (int64_t)1 << 32;   // of a grid, none of its dim
 
 bool too_large(const ksa_params *p, int64_t total_rows, const KsaPagedPlan &plan) {
     if (plan.n_splits > 1 && total_rows * p->n_q_heads * (plan.n_splits > 8 ? 256 : 64) >= MOST_LANES) return true;
-    return !plan.few && (int64_t)plan.slots * plan.n_splits * p->n_kv_heads * plan.pairs * 2 >= MOST_LANES;
+    return !plan.few && (int64_t)plan.slots * plan.n_splits * p->n_kv_heads * plan.pairs * 2 * plan.groups >= MOST_LANES;
 }
 
 size_t workspace_of(const ksa_params *p, int64_t total_rows, const KsaPagedPlan &plan) {
