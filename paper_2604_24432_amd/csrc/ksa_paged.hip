@@ -153,8 +153,8 @@ __device__ __forceinline__ float raised(const f32x16 &sc, float sum, float m_run
     return m;
 }
 // The scores of 32 keys where not all are seen by all: a lane's are those of keys 8 (g / 4) + 4 h + g % 4.  Bit i of `sees`: the row sees key i, of `none`:
-// it has no page.  (Two vector instructions per score, from bits spread over words; comparing positions took twelve: 3.0 us per tile of
-// 64 keys and 128 pairs against 1.3 where all is seen.)
+// it has no page.  (Two vector instructions per score, from bits spread over words; comparing positions took twelve: a tile of 64 keys and 128 pairs
+// alone on its unit 2.9 us, now 2.1; where all is seen 1.45.)
 __device__ __forceinline__ void hide(f32x16 &sc, unsigned sees, unsigned none, int h) {
     const unsigned see = sees >> (4 * h), gone = none >> (4 * h);
     auto spread = [](unsigned x, int g) { return (unsigned)((int)(x << (31 - 8 * (g / 4) - g % 4)) >> 31); };   // all bits of a word
@@ -183,7 +183,13 @@ __device__ __forceinline__ void add_no_numbers(const FwdArgs &a, int hkv, const 
 // ---- few rows -----------------------------------------------------------------------------------------------------------
 
 // At most 32 pairs.  Every wave has blocks of 32 keys of its own, in LDS of its own: no barriers before the end.  The rows of the next block are
-// on their way while one is worked on.
+// on their way while one is worked on: 64 KB per compute unit, two workgroups on each.  With one pair or 32 the work is the same, so the products cost
+// nothing extra where there are few; references are running maxima.  64 sequences at 128K, 32/8 heads, 8-bit, 2.2 GB 334 us, bf16 634, 6.5 - 6.8 TB/s
+// of the 6.8 that a plain read reaches: bound by HBM.  16 sequences of lengths 1 : 3, 8 rows each, 190 MB, 47 us in four spans: by the longest span and by
+// 250 vector instructions per block, of which 8-bit rows' way to bf16 is 90 (bf16, twice the bytes, 72).  4 sequences, 25 MB 13.4 us in 16 spans of
+// 120 keys: a chain of loads, entry, row, LDS.  One, 315 keys 6.3 us.  Dropped: keys of a tile shared by the waves, with two barriers for each (67 and
+// 189 us for the 16 sequences' 8-bit and bf16), the sum of weights looked at as below (level, with outputs off by 1.35 times their own rounding
+// instead of 1.1), weights in two bf16 parts (1.0, 8 % slower on 8-bit caches).
 constexpr int FEW_WAVES = 4, BLOCK = 32;
 
 template <int D, bool F8>
@@ -261,7 +267,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ksa_paged_few_kernel(const 
         for (int g = 0; g < 16; ++g) o[db][g] = 0.f;
     unsigned char *const own = lds + wave * OWN;
     const int grp = lane >> 4, li = lane & 15;
-    const unsigned char *const k_at = own + r * KROW + h * 16, *const v_at = own + BLOCK * KROW + (4 * (grp >> 1) + (li >> 2)) * VROW + 32 * (grp & 1) + 8 * (li & 3);
+    const unsigned char *const k_at = own + r * KROW + h * 16;
+    const unsigned char *const v_at = own + BLOCK * KROW + (4 * (grp >> 1) + (li >> 2)) * VROW + 32 * (grp & 1) + 8 * (li & 3);
     unsigned char *const put_k_at = own + f_row * KROW + f_piece * (F8 ? 32 : 16), *const put_v_at = own + BLOCK * KROW + f_row * VROW + f_piece * (F8 ? 32 : 16);
     auto put = [&](const u32x4 &x, int e, int i, unsigned char *to) {
         u32x4 y[F8 ? 2 : 1];
@@ -432,6 +439,12 @@ __device__ __forceinline__ Tile tile_of(const FwdArgs &a, int slot) {
 // A step works on one tile of keys in two halves of 32.  What a half does: the scores of its keys, the weights of the half before, and the
 // product with V of the half before that, so that the matrix unit's and the vector unit's work do not wait for each other.
 // GROUPS groups of NW waves, 32 pairs each.  Two groups have the same pairs, each half of the keys, and their results are put together in LDS.
+// 2048 rows over 64K keys, 32/8 heads (8 waves) 2.0 - 2.07 ms, 1.07 PFLOP/s, of the 1.36 that a library product of 16384^3 reaches: matrix unit busy 51 % at
+// 2.0 GHz under the power cap, seven vector instructions per MFMA; 4608 rows over 19000 keys, 8-bit, 1.03 - 1.06 ms.  8 waves take a tile from L2 half as often
+// as 4 (2.29 ms).  With one wave per SIMD issue is the bound (a half has 100 vector, 16 matrix, 25 LDS instructions and 20 waits): 1.45 us per tile,
+// two groups 0.85.  Start and end are 6 us: sequence, entries, rows and q one behind the other 3.2, the first tile 1.7, results 1.2.  Dropped: 64 pairs per
+// wave with accumulators in AGPRs (one wave per SIMD, 2.96 ms), operands read further ahead (level), rows asked for half a step ahead (8 x 100 rows in
+// one span 111 us, now 91).
 template <int D, bool F8, int NW, int GROUPS>
 __global__ __launch_bounds__(NW * GROUPS * 64, 2) void ksa_paged_many_kernel(const FwdArgs a) {
     constexpr int KS = D / 16, DB = D / 32, ES = F8 ? 1 : 2, PAIRS = NW * 32;
@@ -443,7 +456,8 @@ __global__ __launch_bounds__(NW * GROUPS * 64, 2) void ksa_paged_many_kernel(con
     constexpr int OWN = 2 * (K_BYTES + V_BYTES);   // of a group: two buffers of K, two of V
     static_assert(NW * 32 * STAGE_ROW <= OWN && (GROUPS == 1 || NW * 64 * (16 * DB + 2) * 4 <= OWN), "the results pass through the tiles' memory");
     __shared__ __align__(16) unsigned char sh_tiles[GROUPS * OWN];
-    __shared__ __align__(16) unsigned sh_states[GROUPS][2][NW];   // of the K tile: which of a wave's rows have no page; bit 31: of the V tile before: elements were taken out
+    // of the K tile: which of a wave's rows have no page; bit 31: of the V tile before: elements were taken out
+    __shared__ __align__(16) unsigned sh_states[GROUPS][2][NW];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6) % NW, group = __builtin_amdgcn_readfirstlane(tid >> 6) / NW;
     const int r = lane & 31, h = lane >> 5;
@@ -797,8 +811,9 @@ __global__ __launch_bounds__(NW * GROUPS * 64, 2) void ksa_paged_many_kernel(con
 
 // ---- the spans' records joined by log-sum-exp -------------------------------------------------------------------------------
 
-// At most MOST spans: D / 4 lanes per (row, query head), every span's record (the last one's again for those behind it) on its way before the
-// row's sequence is looked up.
+// Bound by the records' bytes and, for few of them, by three loads one behind the other.  At most MOST spans: D / 4 lanes per (row, query head), every
+// span's record (the last one's again for those behind it) on its way before the row's sequence is looked up: 20480 items of two spans 7.0 us (a wave for
+// each 11.7; 8 records loaded by branches 18), 128 items 4.1.
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 template <int D, int MOST>
 __global__ __launch_bounds__(256) void ksa_paged_join_few_kernel(const FwdArgs a) {

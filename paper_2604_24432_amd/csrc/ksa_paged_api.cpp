@@ -80,10 +80,10 @@ int64_t most_keys(const ksa_params *p, int64_t rows) {
  * their keys from memory half as often.  The kind and the spans are chosen by what they are expected to take: a start and an end, the key tiles of
  * a span one after the other, rounds where there are more workgroups than places, and for the records of several spans a second kernel.  Per key
  * tile of head_dim 128: 128 pairs 1.5 alone on a unit, 1.95 in pairs, two groups 1.0, 256 pairs 1.75.  Measured, spans each (128 | two groups | 256):
- * full attention, 2048 rows, 64K keys, 32/8 heads 1 2160 | - | 1990; 512 rows 4 575, 8 608 | 2 562, 4 589 | 3 584, 4 520, 8 557; summaries, 512 rows, 4700
- * keys 1 94, 4 55 | 1 71, 2 52 | 3 57, 4 52; 2304 rows, 2000 keys 1 56, 2 82 | 1 71 | 1 67; 2048 rows, 10000 keys 1 281 | 1 290 | 1 258, 2 278; 8 x 100 rows, 4200
- * keys 1 91, 4 46, 6 49 | 1 69, 2 46 | 3 55; window of 1023, 1280 rows, 16/16 heads 1 37, 3 35 | 1 32, 2 49 | 3 37; 2595 rows of six sequences, 2700 keys, 12/4
- * heads, head_dim 64 1 49, 2 39 | 1 39 | 3 46; 64 rows, 830 keys, 8/4 heads 1 20, 6 12.3 | 6 13.3 | 6 13.4.  Over twelve such calls what is chosen takes 1 %
+ * full attention, 2048 rows, 64K keys, 32/8 heads 1 2292 | - | 1 2067; 512 rows 4 614, 8 649 | 2 603, 4 637 | 3 620, 4 562, 8 591; summaries, 512 rows, 4700
+ * keys 1 99, 4 57 | 1 75, 2 54 | 3 60, 4 54; 2304 rows, 2000 keys 1 58, 2 84 | 1 72 | 1 69; 2048 rows, 10000 keys 1 294 | 1 304 | 1 269, 2 296; 8 x 100 rows, 4200
+ * keys 1 91, 4 47, 6 51 | 1 69, 2 47 | 3 57; window of 1023, 1280 rows, 16/16 heads 1 39, 3 36 | 1 34, 2 50 | 3 38; 2595 rows of six sequences, 2700 keys, 12/4
+ * heads, head_dim 64 1 52, 2 41 | 1 41 | 3 48; 64 rows, 830 keys, 8/4 heads 1 20, 6 12.3 | 6 13.3 | 6 13.5.  Over twelve such calls what is chosen takes 1.4 %
  * longer than the best of the three kinds with 1, 2, 3, 4, 6, 8 and 12 spans; without the second kind 3 %.
  */
 KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_rows, int32_t n_splits) {
