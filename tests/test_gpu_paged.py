@@ -103,6 +103,28 @@ def test_many_rows(case, fp8):
         check_attention(p, page, fp8, first, count, 12, n_splits)
 
 
+# (..., text tokens to reckon with, first new row, new rows): enough rows and keys for the largest query tiles, and few rows with many keys
+LARGE = [
+    (32, 2, 128, 64, 0, 4096, 32, 4096, [333, 0], [1100, 1000]),
+    (32, 4, 64, 64, 0, 4096, 16, 4096, [100], [2100]),
+    (30, 3, 128, 16, 4, 8, 16, 16384, [700, 0, 50, 400], [1000, 1, 900, 801]),
+    (48, 4, 64, 16, 4, 8, 64, 16384, [700, 0, 3], [1000, 900, 201]),
+    (32, 2, 128, 1, 0, 700, 16, 4096, [1000, 30], [1200, 1000]),
+    (4, 4, 128, 1, 0, 900, 8, 4096, [1500, 30], [300, 177]),
+    (4, 2, 64, 16, 4, 8, 16, 16384, [3500, 0], [100, 90]),
+]
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("case", LARGE)
+def test_large_tiles_and_long_lists(case, fp8):
+    Hq, Hkv, d, c, m, C, page, n, first, count = case
+    say(f"paged large tiles {case} fp8={fp8}")
+    p = K.make_params(len(first), n, c, m, C, Hq, Hkv, d)
+    for n_splits in (1, 2, 0):
+        check_attention(p, page, fp8, first, count, 18, n_splits, max(count))
+
+
 @pytest.mark.parametrize("rows", [1, 40])
 def test_summary_rows_that_see_only_themselves(rows):
     say(f"paged self-only rows={rows}")
@@ -315,6 +337,52 @@ def test_no_number_reaches_a_row_that_does_not_see_it(rows, n_splits, value, fp8
         assert not bool(torch.isfinite(o[sees][:, 2:, 33].float()).any())
         o[:, 2:, 33] = o0[:, 2:, 33]
         assert torch.equal(bits(o), bits(o0))                                     # the other columns
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("heads,kv_heads,d,rows", [(64, 2, 128, 1100), (4, 2, 128, 300), (64, 2, 64, 1100), (4, 2, 64, 300)])
+def test_no_number_and_no_page_in_large_tiles(heads, kv_heads, d, rows, fp8):
+    """As above and below, in the largest query tiles and where two groups of waves share the keys."""
+    say(f"paged no numbers, large tiles {heads}/{kv_heads} d={d} rows={rows} fp8={fp8}")
+    p = K.make_params(1, 16384, 16, 2, 2, heads, kv_heads, d)
+    first = 1233
+    n = first + rows
+    pages = Pages(p, [n], 8, fp8, 5)
+    k, v = randn(n, kv_heads, d, seed=6), randn(n, kv_heads, d, seed=7)
+    q = randn(rows, heads, d, seed=8)
+    cu, start = batch_of([first], [rows])
+    from tests.paged import kinds, mask
+    see = mask(np.arange(first, n), n, 16, 2, 2)
+    G = heads // kv_heads
+    pages.put(0, 0, k, v)
+    o0, lse0 = K.ksa_paged_fwd(pages.cache, q, cu, start, n_splits=1)
+    assert bool(torch.isfinite(o0.float()).all())
+    for at, of_v in ((n - 1 - rows // 2, False), (n - rows // 3, True), (first - 3, True), (17, True)):
+        sees = torch.from_numpy(see[:, at]).cuda()
+        bad = (v if of_v else k).clone()
+        bad[at, 0, 5] = math.nan
+        pages.put(0, 0, *((k, bad) if of_v else (bad, v)))
+        o, lse = K.ksa_paged_fwd(pages.cache, q, cu, start, n_splits=1)
+        assert torch.equal(bits(o[:, G:]), bits(o0[:, G:])) and torch.equal(lse[:, G:], lse0[:, G:])
+        assert torch.equal(bits(o[~sees]), bits(o0[~sees])) and torch.equal(lse[~sees], lse0[~sees])
+        if of_v:
+            assert bool(torch.isnan(o[sees][:, :G, 5].float()).all()) and torch.equal(lse, lse0)
+            rest = [x for x in range(d) if x != 5]
+            assert torch.equal(bits(o[:, :, rest]), bits(o0[:, :, rest]))
+        else:
+            assert bool(torch.isnan(o[sees][:, :G].float()).all()) and bool(torch.isnan(lse[sees][:, :G]).all())
+    pages.put(0, 0, k, v)
+    _, text, idx = kinds(n, 16, 2)
+    for of_text in (True, False):
+        page = int(idx[n - rows // 2]) // 8 if of_text else 3
+        gone = text & (idx // 8 == page) if of_text else ~text & (idx // 8 == page)
+        table, host = (pages.text_dev, pages.text) if of_text else (pages.sums_dev, pages.sums)
+        table[0, page] = -1
+        o, lse = K.ksa_paged_fwd(pages.cache, q, cu, start, n_splits=1)
+        table.copy_(host)
+        sees = torch.from_numpy((see & gone).any(1)).cuda()
+        assert bool(torch.isnan(o[sees].float()).all()) and bool(torch.isnan(lse[sees]).all())
+        assert torch.equal(bits(o[~sees]), bits(o0[~sees])) and torch.equal(lse[~sees], lse0[~sees])
 
 
 @pytest.mark.parametrize("fp8", [False, True])
