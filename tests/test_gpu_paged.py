@@ -738,3 +738,37 @@ def test_a_cache_keeps_its_own_parameters():
     K.ksa_paged_append(pages.cache, k, k, cu, start)
     k2, _ = K.ksa_paged_read(pages.cache, cu, start, 100)
     assert torch.equal(bits(k2), bits(k))
+
+
+def test_python_refuses_what_does_not_fit():
+    p = K.make_params(2, 1024, 16, 2, 1, 4, 2, 64)
+    pages = Pages(p, [100, 50], 8, True, 5)
+    c = pages.cache
+    half = torch.zeros(10, 2, 64, dtype=torch.bfloat16, device="cuda")
+    q = torch.zeros(10, 4, 64, dtype=torch.bfloat16, device="cuda")
+    cu, start = batch_of([0, 0], [6, 4])
+    k, v, t, u, ke, ve = pages.k, pages.v, pages.text_dev, pages.sums_dev, pages.k_exp, pages.v_exp
+    for make in (lambda: K.PagedCache(p, k, v, t, u), lambda: K.PagedCache(p, k, v, t, u, ke), lambda: K.PagedCache(p, k, v, t, None, ke, ve),
+                 lambda: K.PagedCache(p, k.float(), v.float(), t, u), lambda: K.PagedCache(p, k, v[1:], t, u, ke, ve),
+                 lambda: K.PagedCache(p, k, v.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3), t, u, ke, ve),
+                 lambda: K.PagedCache(p, k, v, t[:1], u, ke, ve), lambda: K.PagedCache(p, k, v, t.long(), u, ke, ve),
+                 lambda: K.PagedCache(p, k, v, t[:, ::2], u, ke, ve), lambda: K.PagedCache(p, k, v, t.cpu(), u, ke, ve),
+                 lambda: K.PagedCache(p, k, v, t, u, ke[1:], ve), lambda: K.PagedCache(p, k.cpu(), v, t, u, ke, ve)):
+        with pytest.raises(ValueError):
+            make()
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    for call in (lambda: K.ksa_paged_append(c, half.float(), half, cu, start), lambda: K.ksa_paged_append(c, half[:, :1], half[:, :1], cu, start),
+                 lambda: K.ksa_paged_append(c, half, half[:9], cu, start), lambda: K.ksa_paged_append(c, half, half, cu[:2], start),
+                 lambda: K.ksa_paged_append(c, half, half, cu, start.long()), lambda: K.ksa_paged_append(c, half, half, cu.cpu(), start),
+                 lambda: K.ksa_paged_append(c, half, half.cpu(), cu, start), lambda: K.ksa_paged_append(c, half, q[:, ::2], cu, start),
+                 lambda: K.ksa_paged_read(c, cu, start, 9, k=half), lambda: K.ksa_paged_read(c, cu, start, 10, k=half, v=q[:, ::2]),
+                 lambda: K.ksa_paged_fwd(c, half, cu, start), lambda: K.ksa_paged_fwd(c, q[..., ::2], cu, start),
+                 lambda: K.ksa_paged_fwd(c, q, cu, start, o=q.float()), lambda: K.ksa_paged_fwd(c, q, cu, start, lse=torch.zeros(4, 10, device="cuda")),
+                 lambda: K.ksa_paged_fwd(c, q, cu, start, workspace=ws.float()), lambda: K.ksa_paged_fwd(c, q, cu, start, workspace=ws.cpu())):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: K.ksa_paged_fwd(c, q, cu, start, n_splits=-1), lambda: K.ksa_paged_fwd(c, q, cu, start, max_rows=0),
+                 lambda: K.ksa_paged_fwd(c, q, cu, start, n_splits=2, workspace=ws[:16]), lambda: K.ksa_paged_fwd(c, q, cu, start, n_splits=2, workspace=ws[1:]),
+                 lambda: K.ksa_paged_fwd(c, torch.cat([q, q]).as_strided((10, 4, 64), (260, 64, 1)), cu, start, o=torch.empty_like(q))):
+        with pytest.raises(K.KsaError):
+            call()
