@@ -440,7 +440,7 @@ __device__ __forceinline__ Tile tile_of(const FwdArgs &a, int slot) {
 // product with V of the half before that, so that the matrix unit's and the vector unit's work do not wait for each other.
 // GROUPS groups of NW waves, 32 pairs each.  Two groups have the same pairs, each half of the keys, and their results are put together in LDS.
 // 2048 rows over 64K keys, 32/8 heads (8 waves) 2.0 - 2.07 ms, 1.07 PFLOP/s, of the 1.36 that a library product of 16384^3 reaches: matrix unit busy 51 % at
-// 2.0 GHz under the power cap, seven vector instructions per MFMA; 4608 rows over 19000 keys, 8-bit, 1.03 - 1.06 ms.  8 waves take a tile from L2 half as often
+// 2.0 GHz under the power cap, seven vector instructions per MFMA; 4608 rows over 19000 keys, 8-bit, 1.02 - 1.08 ms.  8 waves take a tile from L2 half as often
 // as 4 (2.29 ms).  With one wave per SIMD issue is the bound (a half has 100 vector, 16 matrix, 25 LDS instructions and 20 waits): 1.45 us per tile,
 // two groups 0.85.  Start and end are 6 us: sequence, entries, rows and q one behind the other 3.2, the first tile 1.7, results 1.2.  Dropped: 64 pairs per
 // wave with accumulators in AGPRs (one wave per SIMD, 2.96 ms), operands read further ahead (level), rows asked for half a step ahead (8 x 100 rows in

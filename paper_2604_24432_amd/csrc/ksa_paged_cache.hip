@@ -1,7 +1,7 @@
 // Rows into and out of the paged cache, as bf16 or as e4m3 numbers with one power of two per row and KV head.  Data movement, bound by
 // HBM: 16 bytes of a row per lane, the row's largest magnitude by lane moves, the table looked up by every row's lanes.  36864 rows, 8 heads,
-// d 128, 8-bit: in 58 us and out again 34, 454 MB at 4.9 TB/s (a copy on this card 5.0); 54000 rows, 16 heads, bf16, out 100 us, 5.3 TB/s; 64 rows
-// of 64 sequences 3.1 us, a launch and three loads one behind the other.  Loads of the new rows in front of the lookup (in 61 / 3.3 us),
+// d 128, 8-bit: in 56 us and out again 34, 454 MB at 5.0 TB/s (a copy on this card 5.0); 54000 rows, 16 heads, bf16, out 100 us, 5.3 TB/s; 64 rows
+// of 64 sequences 2.8 us, a launch and three loads one behind the other.  Loads of the new rows in front of the lookup (in 61 / 3.3 us),
 // two or four rows per lane (66 / 3.9, 69 / 5.0) did not pay.
 #include <hip/hip_runtime.h>
 
