@@ -328,7 +328,8 @@ int ksa_decode_summary_fwd(const ksa_params *params /*host*/, const void *q, con
  * KSA_CACHE_FP8 holds a row of one KV head as 8-bit floats (e4m3: 4 significant bits, largest 448) times a power of two 2^e:
  * e is the least integer in [-117, 119] with max |x| <= 448 * 2^e over the row's finite elements (119 if none is), every element is x / 2^e rounded
  * to the nearest e4m3 number (ties to even; what lies beyond 448 * 2^119 = 2.98e38 becomes that), infinities and NaN become
- * NaN.  k_exp and v_exp hold e + 127.  What a row stands for is zero or a normal bf16 number per element: reading it back and attending to it
+ * NaN.  k_exp and v_exp hold e + 127.  With a byte there that is none of those (in a slot never written) the rows that see it may come out as
+ * anything, and only they.  What a row stands for is zero or a normal bf16 number per element: reading it back and attending to it
  * add no rounding.
  */
 #define KSA_CACHE_BF16 0

@@ -38,6 +38,11 @@ struct FwdArgs {
 
 constexpr float LOWEST = -FLT_MAX;
 
+// Largest exponent byte of the 8-bit format.  Where a key is not seen by every row a larger one of its V row counts as this one, so that the row is
+// finite (448 * 2^119 is a bf16 number) and a weight of zero keeps it out of a sum.  Slots that were never written hold such bytes: what is read
+// in a missing page's place, summaries that are listed and seen by no row, and rows that only others see.
+constexpr int MOST_EXP = 127 + 119;
+
 // value of lane l ^ 32
 __device__ __forceinline__ float swap32(float x) {
     const unsigned u = __builtin_bit_cast(unsigned, x);
@@ -282,7 +287,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ksa_paged_few_kernel(const 
         const unsigned none = lost;
         const bool whole = none == 0 && sees_all(x);
         if (!whole) {
-            if (F8) ve = (none >> r) & 1 ? 127 : ve;   // (without a page: any exponent)
+            if (F8) ve = min(ve, MOST_EXP);
             bool odd = false;
 #pragma unroll
             for (int i = 0; i < NI; ++i) odd |= take_out_raw<F8>(vr[i]);
@@ -529,7 +534,7 @@ __global__ __launch_bounds__(NW * GROUPS * 64, 2) void ksa_paged_many_kernel(con
         if constexpr (F8) next_k_e = a.k_exp[exp_at], next_v_e = a.v_exp[exp_at];
     };
     auto take_exps = [&]() {   // (a step after they were asked for)
-        if constexpr (F8) k_e = next_k_e, v_e = lost ? 127 : next_v_e;   // (without a page: any exponent)
+        if constexpr (F8) k_e = next_k_e, v_e = min(next_v_e, MOST_EXP);
     };
     auto load_k = [&](int i) { k_rows[i] = *reinterpret_cast<const u32x4 *>(kb + from[i]); };
     auto load_v = [&](int i) { v_rows[i] = *reinterpret_cast<const u32x4 *>(vb + from[i]); };

@@ -91,7 +91,8 @@ KSA_INDEX Keys keys_between(const Visible &first, const Visible &last) {
     const int n_s = max(last.hi_s - first.lo_s, 0);
     return {first.lo_s, n_s, first.lo_t, n_s + last.hi_t - first.lo_t};
 }
-// ... of the augmented rows from .. to (both included)
+// ... of the augmented rows from .. to (both included).  Summaries between those that the text rows see and those that the summary rows see, up to C m,
+// are listed too, though no row sees them.
 KSA_INDEX Keys keys_of(const PagedRows &a, int from, int to) {
     const int c = a.c, m = a.m, w = c + m;
     const int j0 = ksa_div(from, a.by_w), r0 = from - j0 * w, j1 = ksa_div(to, a.by_w), r1 = to - j1 * w;
