@@ -379,7 +379,8 @@ int ksa_paged_read(const ksa_params *params /*host*/, const ksa_paged_cache *cac
                    const int64_t kv_strides[2], const int32_t *cu_rows, const int32_t *start, int64_t total_rows, void *stream);
 
 /* Bytes of device workspace ksa_paged_fwd needs for total_rows new rows, at most max_rows of one sequence, and this number of key splits
- * (0 = library default); 0 also for arguments that make no sense. */
+ * (0 = library default, for which it is what the fastest number takes: few rows may take more than many, which are cut into fewer spans); 0 also
+ * for arguments that make no sense. */
 size_t ksa_paged_workspace_bytes(const ksa_params *params /*host*/, int64_t total_rows, int64_t max_rows, int32_t n_splits);
 
 /*
@@ -389,10 +390,11 @@ size_t ksa_paged_workspace_bytes(const ksa_params *params /*host*/, int64_t tota
  *   q, o: device bf16 [total_rows, Hq, d]; lse: device fp32 [total_rows, Hq] contiguous, natural-log sum-exp of the scaled
  *   visible scores, or NULL.  o may be the memory of q (same strides).
  *   max_rows: no sequence has more new rows; one that has is out of place.  It sizes the launch.
- *   workspace: device, 16-byte aligned, at least ksa_paged_workspace_bytes(params, total_rows, max_rows, n_splits) bytes (NULL if that is 0),
+ *   workspace: device, 16-byte aligned, at least ksa_paged_workspace_bytes(params, total_rows, max_rows, n_splits) bytes (NULL if that is 0); with
+ *   n_splits = 0 it may hold less (NULL and 0 bytes among it): the library then takes no more spans than it holds.  It is
  *   needed until the work enqueued on `stream` has finished; calls that share one must be stream-ordered.
  *   n_splits: spans that the keys of a sequence are cut into, each read by workgroups of its own; 0: the library chooses (by params->n_text,
- *   the context that it must reckon with), else 1 .. 1024.
+ *   the context that it must reckon with, and the workspace), else 1 .. 1024.  Another number of them rounds differently.
  * Scores, maxima and sums are fp32; weights are rounded to bf16 for P V.  A row's outputs depend on nothing that it does not see:
  * infinities and NaN elsewhere do not reach it.  No atomics.
  * Errors also: WORKSPACE_TOO_SMALL.

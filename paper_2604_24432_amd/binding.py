@@ -699,7 +699,8 @@ def ksa_paged_fwd(cache: PagedCache, q, cu_rows, start, max_rows: Optional[int] 
                   n_splits: int = 0, stream=None):
     """q [rows, Hq, d] bf16, the queries of the rows that ksa_paged_append wrote -> o like q, lse [rows, Hq] fp32.
     max_rows: the largest number of rows of a sequence (all of them if omitted); workspace: uint8, at least
-    paged_workspace_bytes(cache, rows, max_rows, n_splits) bytes (allocated here if omitted).  What is allocated here belongs to `stream`."""
+    paged_workspace_bytes(cache, rows, max_rows, n_splits) bytes (allocated here if omitted; with n_splits = 0 a smaller one, of any size, means
+    fewer spans).  What is allocated here belongs to `stream`."""
     import torch
     if stream is not None and (o is None or workspace is None or lse is None and return_lse):
         _check_stream(cache, stream)

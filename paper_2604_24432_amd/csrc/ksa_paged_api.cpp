@@ -85,8 +85,11 @@ int64_t most_keys(const ksa_params *p, int64_t rows) {
  * keys 1 91, 4 47, 6 51 | 1 69, 2 47 | 3 57; window of 1023, 1280 rows, 16/16 heads 1 39, 3 36 | 1 34, 2 50 | 3 38; 2595 rows of six sequences, 2700 keys, 12/4
  * heads, head_dim 64 1 52, 2 41 | 1 41 | 3 48; 64 rows, 830 keys, 8/4 heads 1 20, 6 12.3 | 6 13.3 | 6 13.5.  Over twelve such calls what is chosen takes 1.4 %
  * longer than the best of the three kinds with 1, 2, 3, 4, 6, 8 and 12 spans; without the second kind 3 %.
+ *
+ * most: what is chosen here has at most so many spans.
  */
-KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_rows, int32_t n_splits) {
+constexpr int64_t MOST_SPANS = 64;
+KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_rows, int32_t n_splits, int64_t most = MOST_SPANS) {
     const int32_t group = p->n_q_heads / p->n_kv_heads;
     KsaPagedPlan plan = {false, n_splits, 0, 0, 0};
     if (max_rows * group <= KSA_PAGED_FEW) {
@@ -95,7 +98,7 @@ KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_row
         if (n_splits != 0) return plan;
         const int64_t keys = most_keys(p, max_rows);
         const int64_t least = units >= 128 ? 512 : units >= 64 ? 256 : 128;
-        plan.n_splits = keys < 512 ? 1 : (int32_t)std::max<int64_t>(1, std::min({512 / units, keys / least, (int64_t)64}));
+        plan.n_splits = keys < 512 ? 1 : (int32_t)std::max<int64_t>(1, std::min({512 / units, keys / least, most}));
         return plan;
     }
     const double size = p->head_dim == 128 ? 1.0 : 0.7;
@@ -112,7 +115,7 @@ KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_row
         const double rows = (double)total_rows * p->chunk_len / (p->chunk_len + p->n_summary);
         const double full = rows * group / pairs, units = (p->batch == 1 ? std::ceil(full) : full + 0.5 * p->batch) * p->n_kv_heads;
         const int64_t tiles = (most_keys(p, std::min<int64_t>(max_rows, pairs / group + 1)) + 63) / 64;
-        for (int32_t n = n_splits == 0 ? 1 : n_splits; n <= (n_splits == 0 ? 64 : n_splits); ++n) {
+        for (int32_t n = n_splits == 0 ? 1 : n_splits; n <= (n_splits == 0 ? most : n_splits); ++n) {
             if (n_splits == 0 && n > 1 && n > tiles) break;
             const bool two = pairs == 128 && kind.groups == 1;   // on a compute unit
             const double places = two ? 512 : 256, wgs = units * n;
@@ -134,8 +137,9 @@ bool too_large(const ksa_params *p, int64_t total_rows, const KsaPagedPlan &plan
     return !plan.few && (int64_t)plan.slots * plan.n_splits * p->n_kv_heads * plan.pairs * 2 * plan.groups >= MOST_LANES;
 }
 
+size_t span_bytes(const ksa_params *p, int64_t total_rows) { return (size_t)total_rows * p->n_q_heads * ksa_paged_record(p->head_dim) * sizeof(float); }
 size_t workspace_of(const ksa_params *p, int64_t total_rows, const KsaPagedPlan &plan) {
-    return plan.n_splits == 1 ? 0 : (size_t)total_rows * p->n_q_heads * plan.n_splits * ksa_paged_record(p->head_dim) * sizeof(float);
+    return plan.n_splits == 1 ? 0 : plan.n_splits * span_bytes(p, total_rows);
 }
 
 int move_call(KsaPagedMove &a, const ksa_params *p, const ksa_paged_cache *cache, const void *k, const void *v, const int64_t *strides,
@@ -199,7 +203,8 @@ int ksa_paged_fwd(const ksa_params *p, const ksa_paged_cache *cache, const void 
     if ((rc = check_strides(a.o_strides, o_strides, p->n_q_heads, p->head_dim)) != KSA_OK) return rc;
     if (total_rows == 0) return KSA_OK;
     a.max_rows = (int32_t)std::min(max_rows, total_rows);
-    a.plan = plan_paged(p, total_rows, a.max_rows, n_splits);
+    const size_t room = std::min<size_t>(workspace_bytes / span_bytes(p, total_rows), MOST_SPANS);
+    a.plan = plan_paged(p, total_rows, a.max_rows, n_splits, std::max<int64_t>(room, 1));
     if (too_large(p, total_rows, a.plan)) return KSA_ERR_UNSUPPORTED;
     const size_t need = workspace_of(p, total_rows, a.plan);
     if (need > 0 && !workspace) return KSA_ERR_INVALID_ARG;

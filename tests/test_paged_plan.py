@@ -1,0 +1,70 @@
+"""How ksa_paged_fwd deals a call to workgroups (plan_paged in ksa_paged_api.cpp; no GPU needed)."""
+import os
+import random
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2604_24432_amd", "csrc")
+INVALID, TOO_SMALL = -1, -3
+
+
+@pytest.fixture(scope="module")
+def plans(tmp_path_factory):
+    """Of a list of (batch, heads, KV heads, d, tokens, c, m, C, new rows, most of a sequence, spans, bytes of workspace or -1)."""
+    exe = str(tmp_path_factory.mktemp("plan") / "paged_plan")
+    subprocess.run(["g++", "-O1", "-std=c++17", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+                    os.path.join(ROOT, "tests", "plan", "paged_plan.cpp"), os.path.join(CSRC, "ksa_paged_api.cpp"), os.path.join(CSRC, "ksa_layout.cpp"),
+                    "-o", exe], check=True)
+
+    def run(calls):
+        out = subprocess.run([exe], input="\n".join(" ".join(map(str, c)) for c in calls), capture_output=True, text=True)
+        assert out.returncode == 0, out.stderr[-2000:]
+        return [dict(zip(("status", "few", "n_splits", "pairs", "groups", "slots", "bytes"), map(int, line.split()))) for line in out.stdout.splitlines()]
+    return run
+
+
+def random_calls(count, seed):
+    rng = random.Random(seed)
+    for _ in range(count):
+        c, m, C = rng.choice([(64, 8, 1), (8, 1, 128), (16, 2, 64), (48, 6, 2), (1, 0, 1023), (64, 0, 4096)])
+        kv_heads = rng.choice([1, 2, 3, 4, 8, 16])
+        batch, most = rng.choice([1, 1, 2, 3, 8, 16, 64, 150]), rng.choice([1, 1, 4, 8, 33, 300, 2048])
+        yield (batch, kv_heads * rng.choice([1, 2, 4, 8]), kv_heads, rng.choice([64, 128]), int(10 ** rng.uniform(2.5, 5.5)), c, m, C,
+               rng.randint(1, batch * most), most, 0, -1)
+
+
+def test_a_smaller_workspace_means_fewer_spans(plans):
+    """A call that leaves the spans to the library takes any workspace: one sized for another call's rows, the least, none at all."""
+    rng = random.Random(1)
+    calls = list(random_calls(3000, 1))
+    asked = plans(calls)
+    assert all(x["status"] == 0 for x in asked) and sum(x["n_splits"] > 1 for x in asked) > 500
+    for given in (lambda n: 0, lambda n: n // 2, lambda n: n - 1, lambda n: rng.randint(0, n), lambda n: n, lambda n: 2 * n + 100):
+        sizes = [given(x["bytes"]) for x in asked]
+        for c, want, size, got in zip(calls, asked, sizes, plans([(*c[:-1], max(n, 0)) for c, n in zip(calls, sizes)])):
+            per_span = c[8] * c[1] * (c[3] + 4) * 4
+            assert got["status"] == 0, (c, size, got)
+            assert got["n_splits"] == 1 or got["n_splits"] * per_span <= size
+            if size >= want["bytes"]:
+                assert got == want
+            elif got["few"]:
+                assert got["n_splits"] == max(1, size // per_span)     # as many as it holds
+
+
+def test_one_workspace_for_all_batches_of_a_serving_loop(plans):
+    """64K tokens, 8 sequences: 8192 rows need no workspace, 512 and 64 would have some."""
+    many, some, few = plans([(8, 32, 8, 128, 65536, 64, 8, 1, n, 2048, 0, -1) for n in (8192, 512, 64)])
+    assert many["bytes"] == 0 < few["bytes"] < some["bytes"]
+    for n in (512, 64):
+        for size in (0, few["bytes"]):
+            got, = plans([(8, 32, 8, 128, 65536, 64, 8, 1, n, 2048, 0, size)])
+            assert got["status"] == 0
+
+
+def test_a_number_of_spans_that_was_asked_for_needs_its_workspace(plans):
+    for n, bytes_of in ((2, 64 * 32 * 2 * 132 * 4), (1024, 64 * 32 * 1024 * 132 * 4)):
+        call = (64, 32, 8, 128, 4096, 64, 8, 1, 64, 1, n)
+        exact, less, none = plans([(*call, bytes_of), (*call, bytes_of - 1), (*call, 0)])
+        assert (exact["status"], less["status"], none["status"]) == (0, TOO_SMALL, INVALID) and exact["n_splits"] == n
