@@ -400,7 +400,7 @@ int ksa_validate_params(const ksa_params *p) {
     if (p->flags & ~KSA_FLAG_SUMMARY_SELF_ONLY) return KSA_ERR_INVALID_ARG;
     if (!(p->softmax_scale == p->softmax_scale)) return KSA_ERR_INVALID_ARG;  // NaN
     // an incomplete last chunk has text positions only (its summaries do not exist yet)
-    const int64_t L = (int64_t)(p->n_text / p->chunk_len) * (p->chunk_len + p->n_summary) + p->n_text % p->chunk_len;
+    const int64_t L = (p->n_text / p->chunk_len) * ((int64_t)p->chunk_len + p->n_summary) + p->n_text % p->chunk_len;
     if (L >= (int64_t)1 << 30) return KSA_ERR_UNSUPPORTED;  // row indices are int32 on the device
     if (p->batch > 65535 || p->n_q_heads > 65535) return KSA_ERR_UNSUPPORTED;
     if (p->head_dim != 64 && p->head_dim != 128) return KSA_ERR_UNSUPPORTED;

@@ -59,7 +59,8 @@ inline PagedRows paged_rows(const KsaPagedCall &L) {
     a.text_cols = L.cache.text_pages, a.sum_cols = L.p.n_summary > 0 ? L.cache.summary_pages : 0;
     a.n_pages = L.cache.n_pages, a.shift = L.page_shift;
     a.cu = L.cu_rows, a.start = L.start, a.batch = L.p.batch, a.total = L.total_rows, a.aug_len = L.aug_len;
-    a.c = L.p.chunk_len, a.m = L.p.n_summary, a.C = L.p.window_chunks, a.self_only = (L.p.flags & KSA_FLAG_SUMMARY_SELF_ONLY) ? 1 : 0;
+    // (where no chunk is ever whole there are no summaries, and c + m, which may exceed 32 bits then, is c)
+    a.c = L.p.chunk_len, a.m = L.p.chunk_len > L.p.n_text ? 0 : L.p.n_summary, a.C = L.p.window_chunks, a.self_only = (L.p.flags & KSA_FLAG_SUMMARY_SELF_ONLY) ? 1 : 0;
     a.by_w = ksa_divisor(a.c + a.m), a.by_c = ksa_divisor(a.c), a.by_m = ksa_divisor(a.m > 0 ? a.m : 1);
     return a;
 }

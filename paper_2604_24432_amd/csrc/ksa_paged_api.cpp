@@ -9,8 +9,10 @@ namespace {
 
 bool aligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
+// augmented rows of a chunk; one that is longer than every text may exceed 32 bits
+int64_t chunk_rows(const ksa_params *p) { return (int64_t)p->chunk_len + p->n_summary; }
 int64_t augmented(const ksa_params *p) {
-    return (int64_t)(p->n_text / p->chunk_len) * (p->chunk_len + p->n_summary) + p->n_text % p->chunk_len;
+    return (p->n_text / p->chunk_len) * chunk_rows(p) + p->n_text % p->chunk_len;
 }
 
 int check_sizes(const ksa_params *p, int64_t total_rows) {
@@ -112,7 +114,7 @@ KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_row
         // every sequence ends one tile of text and one of summaries before it is full; the latter's lists are short
         const int32_t pairs = kind.pairs;
         const int64_t slots = total_rows * group / pairs + (p->n_summary > 0 ? 2 : 1) * (int64_t)p->batch;
-        const double rows = (double)total_rows * p->chunk_len / (p->chunk_len + p->n_summary);
+        const double rows = (double)total_rows * p->chunk_len / chunk_rows(p);
         const double full = rows * group / pairs, units = (p->batch == 1 ? std::ceil(full) : full + 0.5 * p->batch) * p->n_kv_heads;
         const int64_t tiles = (most_keys(p, std::min<int64_t>(max_rows, pairs / group + 1)) + 63) / 64;
         for (int32_t n = n_splits == 0 ? 1 : n_splits; n <= (n_splits == 0 ? most : n_splits); ++n) {
@@ -161,7 +163,7 @@ int ksa_paged_pages(const ksa_params *p, int32_t page_rows, int64_t n_rows, int6
     if (rc != KSA_OK) return rc;
     if (page_rows < 8 || page_rows > 1024 || (page_rows & (page_rows - 1)) || n_rows < 0) return KSA_ERR_INVALID_ARG;
     if (n_rows > augmented(p)) return KSA_ERR_OUT_OF_RANGE;
-    const int64_t w = p->chunk_len + p->n_summary, text = n_rows / w * p->chunk_len + std::min<int64_t>(n_rows % w, p->chunk_len);
+    const int64_t w = chunk_rows(p), text = n_rows / w * p->chunk_len + std::min<int64_t>(n_rows % w, p->chunk_len);
     if (text_pages) *text_pages = (text + page_rows - 1) / page_rows;
     if (summary_pages) *summary_pages = (n_rows - text + page_rows - 1) / page_rows;
     return KSA_OK;

@@ -68,3 +68,13 @@ def test_a_number_of_spans_that_was_asked_for_needs_its_workspace(plans):
         call = (64, 32, 8, 128, 4096, 64, 8, 1, 64, 1, n)
         exact, less, none = plans([(*call, bytes_of), (*call, bytes_of - 1), (*call, 0)])
         assert (exact["status"], less["status"], none["status"]) == (0, TOO_SMALL, INVALID) and exact["n_splits"] == n
+
+
+def test_chunks_longer_than_any_text(plans):
+    """c + m beyond 32 bits: as with chunks that are a little longer than the text (the host code runs under UBSan here)."""
+    most = 2 ** 31 - 1
+    for n, rows in ((100, 50), (100, 1), (5000, 300)):
+        for d in (64, 128):
+            calls = [(1, 4, 2, d, n, c, m, 1, rows, rows, 0, -1) for c, m in ((10 ** 9, 10 ** 9), (most, most), (10 ** 9, 10 ** 9 // 2), (most - 1, most // 2))]
+            got = plans(calls)
+            assert got[0] == got[1] and got[2] == got[3] and got[0]["status"] == got[2]["status"] == 0
