@@ -78,3 +78,25 @@ def test_chunks_longer_than_any_text(plans):
             calls = [(1, 4, 2, d, n, c, m, 1, rows, rows, 0, -1) for c, m in ((10 ** 9, 10 ** 9), (most, most), (10 ** 9, 10 ** 9 // 2), (most - 1, most // 2))]
             got = plans(calls)
             assert got[0] == got[1] and got[2] == got[3] and got[0]["status"] == got[2]["status"] == 0
+
+
+def test_the_gpu_tests_reach_every_kernel(plans):
+    """Which kernel a call takes is a matter of measured constants: with the present ones the cases of the GPU tests reach all of them, at both head
+    sizes, with one span and with several, and so do the tests of the exponents.  (Tiles of 256 pairs are reached by the first four of LARGE and by none
+    of MANY.)"""
+    from tests.test_gpu_paged import FEW, LARGE, MANY
+    from tests.test_gpu_paged_exponents import TILES
+    calls = []
+    for Hq, Hkv, d, c, m, C, _, first, count in FEW:
+        calls += [(len(first), Hq, Hkv, d, 4096, c, m, C, sum(count), max(count), n, -1) for n in (1, 3, 0)]
+    for Hq, Hkv, d, c, m, C, _, first, count in MANY:
+        calls += [(len(first), Hq, Hkv, d, 4096, c, m, C, sum(count), sum(count), n, -1) for n in (1, 3, 0)]
+    for Hq, Hkv, d, c, m, C, _, n_text, first, count in LARGE:
+        calls += [(len(first), Hq, Hkv, d, n_text, c, m, C, sum(count), max(count), n, -1) for n in (1, 2, 0)]
+    kinds = [(c[3], "few" if x["few"] else (x["pairs"], x["groups"]), x["n_splits"] > 1) for c, x in zip(calls, plans(calls))]
+    every = {(d, kind, several) for d in (64, 128) for kind in ("few", (128, 1), (128, 2), (256, 1)) for several in (False, True)}
+    assert set(kinds) == every, every - set(kinds)
+    of_256 = {c[:3] for c, (_, kind, _) in zip(calls, kinds) if kind == (256, 1)}
+    assert of_256 == {(len(x[8]), *x[:2]) for x in LARGE[:4]}
+    calls = [(1, Hq, Hkv, d, n, 16, 2, 2, rows, rows, n_splits, -1) for Hq, Hkv, d, n, rows, n_splits in TILES]
+    assert {(c[3], "few" if x["few"] else (x["pairs"], x["groups"])) for c, x in zip(calls, plans(calls))} == {x[:2] for x in every}
