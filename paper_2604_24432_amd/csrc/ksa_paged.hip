@@ -132,6 +132,7 @@ __device__ __forceinline__ float log_sum(float m, float l) { return (m + __built
 // is exact in bf16 and the largest one's rounding is what the output keeps of all of them: off by 1.40 times an output's own rounding (4000 keys,
 // half of the scores within 1), with 128 1.22, with 64 1.12.  Time: full attention of 2048 rows over 64K keys 1997 us with 2^20, 2029 with 128, 2067 with 64;
 // window of 1023 30.2, 32.0, 33.2; a running maximum takes eight more vector instructions of a hundred in every half, 64 more where it moves.
+// The sum is of the weights as they are in 32 bits, of which many average their roundings out; the sum of the rounded ones took 4 - 8 %.
 constexpr float HIGH = 128.f;
 
 // Bytes from one row of a tile to the next in LDS: the 16 rows of a phase of the plain reads of K, 16 bytes each, and the 4 rows of one of the
@@ -444,8 +445,9 @@ __device__ __forceinline__ Tile tile_of(const FwdArgs &a, int slot) {
 // A step works on one tile of keys in two halves of 32.  What a half does: the scores of its keys, the weights of the half before, and the
 // product with V of the half before that, so that the matrix unit's and the vector unit's work do not wait for each other.
 // GROUPS groups of NW waves, 32 pairs each.  Two groups have the same pairs, each half of the keys, and their results are put together in LDS.
-// 2048 rows over 64K keys, 32/8 heads (8 waves) 2.0 - 2.07 ms, 1.07 PFLOP/s, of the 1.36 that a library product of 16384^3 reaches: matrix unit busy 51 % at
-// 2.0 GHz under the power cap, seven vector instructions per MFMA; 4608 rows over 19000 keys, 8-bit, 1.02 - 1.08 ms.  8 waves take a tile from L2 half as often
+// 2048 rows over 64K keys, 32/8 heads (8 waves) 1.98 - 2.15 ms, 1.0 - 1.1 PFLOP/s, of the 1.36 that a library product of 16384^3 reaches: seven vector
+// and two LDS instructions per MFMA keep the board at its power cap (2.0 GHz) with the matrix unit busy half of the time; 4608 rows over 19000 keys, 8-bit, 1.02 -
+// 1.11 ms.  8 waves take a tile from L2 half as often
 // as 4 (2.29 ms).  With one wave per SIMD issue is the bound (a half has 100 vector, 16 matrix, 25 LDS instructions and 20 waits): 1.45 us per tile,
 // two groups 0.85.  Start and end are 6 us: sequence, entries, rows and q one behind the other 3.2, the first tile 1.7, results 1.2.  Dropped: 64 pairs per
 // wave with accumulators in AGPRs (one wave per SIMD, 2.96 ms), operands read further ahead (level), rows asked for half a step ahead (8 x 100 rows in

@@ -69,24 +69,44 @@ int64_t most_keys(const ksa_params *p, int64_t rows) {
 }
 
 /*
- * How a call is dealt.  All times in us.
+ * How a call is dealt.  All times in us; spans: time.
  *
  * Few rows: a workgroup per sequence, KV head and span of the keys, about 512 of them (two on each compute unit), and no span below 128 keys, 256
- * from 64 sequences x KV heads on, 512 from 128 on; below 512 keys one span.  Sequences x KV heads, keys: 1, 400 1 7.9, 4 7.5; 1, 700 1 9.6, 4 7.8, 6
- * 7.9; 1, 1200 2 11.1, 6 8.1, 16 8.5; 1, 9000 16 15.5, 32 12.9, 64 11.9; 8, 6000 8 17.3, 24 12.7, 64 13.1; 32, 800 4 11.0, 8 10.4, 16 10.9; 32, 4200 4
- * 21.5, 8 17.6, 16 17.2, 32 21.9; 64, 800 3 12.8, 4 12.0, 6 13.7; 64, 1500 4 15.8, 6 16.4; 128, 9000, 8 rows, 8-bit 2 78.5, 4 53.1, 8 52.3, 16 58.1; 160, 800
- * 1 13.6, 3 15.0; 256, 1500, 4 rows, 8-bit 1 26.2, 2 27.0; 256, 4000 1 57.6, 2 57.2, 4 55.9; 512, 16500 1 636, 2 641, 4 656; 16, 65536, 8 rows 8 99, 16 89,
- * 32 91.  Spans dealt by the sequences' lengths (lengths 1 : 4): 128 57.4, the same number each 53.8; 512 248, 249.
+ * from 64 sequences x KV heads on, 512 from 128 on; below 512 keys one span.
+ *   sequences x KV heads   keys                   measured
+ *                      1    400                   1: 7.9    4: 7.5
+ *                      1    700                   1: 9.6    4: 7.8    6: 7.9
+ *                      1   1200                   2: 11.1   6: 8.1   16: 8.5
+ *                      1   9000                  16: 15.5  32: 12.9  64: 11.9
+ *                      8   6000                   8: 17.3  24: 12.7  64: 13.1
+ *                     32    800                   4: 11.0   8: 10.4  16: 10.9
+ *                     32   4200                   4: 21.5   8: 17.6  16: 17.2  32: 21.9
+ *                     64    800                   3: 12.8   4: 12.0   6: 13.7
+ *                     64   1500                   4: 15.8   6: 16.4
+ *                    128   9000, 8 rows, 8-bit    2: 78.5   4: 53.1   8: 52.3  16: 58.1
+ *                    160    800                   1: 13.6   3: 15.0
+ *                    256   1500, 4 rows, 8-bit    1: 26.2   2: 27.0
+ *                    256   4000                   1: 57.6   2: 57.2   4: 55.9
+ *                    512  16500                   1: 636    2: 641    4: 656
+ *                     16  65536, 8 rows           8: 99    16: 89    32: 91
+ * Spans dealt by the sequences' lengths (lengths 1 : 4) instead of the same number each: 57.4 and 53.8 with 128, 248 and 249 with 512.
  *
  * Many rows: tiles of 128 pairs, two on a compute unit; of 128, alone, whose two groups of waves have half of the keys each; of 256, alone, which take
  * their keys from memory half as often.  The kind and the spans are chosen by what they are expected to take: a start and an end, the key tiles of
  * a span one after the other, rounds where there are more workgroups than places, and for the records of several spans a second kernel.  Per key
- * tile of head_dim 128: 128 pairs 1.5 alone on a unit, 1.95 in pairs, two groups 1.0, 256 pairs 1.75.  Measured, spans each (128 | two groups | 256):
- * full attention, 2048 rows, 64K keys, 32/8 heads 1 2292 | - | 1 2067; 512 rows 4 614, 8 649 | 2 603, 4 637 | 3 620, 4 562, 8 591; summaries, 512 rows, 4700
- * keys 1 99, 4 57 | 1 75, 2 54 | 3 60, 4 54; 2304 rows, 2000 keys 1 58, 2 84 | 1 72 | 1 69; 2048 rows, 10000 keys 1 294 | 1 304 | 1 269, 2 296; 8 x 100 rows, 4200
- * keys 1 91, 4 47, 6 51 | 1 69, 2 47 | 3 57; window of 1023, 1280 rows, 16/16 heads 1 39, 3 36 | 1 34, 2 50 | 3 38; 2595 rows of six sequences, 2700 keys, 12/4
- * heads, head_dim 64 1 52, 2 41 | 1 41 | 3 48; 64 rows, 830 keys, 8/4 heads 1 20, 6 12.3 | 6 13.3 | 6 13.5.  Over twelve such calls what is chosen takes 1.4 %
- * longer than the best of the three kinds with 1, 2, 3, 4, 6, 8 and 12 spans; without the second kind 3 %.
+ * tile of head_dim 128: 128 pairs 1.5 alone on a unit, 1.95 in pairs, two groups 1.0, 256 pairs 1.75.
+ *                                                            128 pairs            two groups     256 pairs
+ *   full attention, 64K keys, 32/8 heads, 2048 rows          1: 2292                             1: 2067
+ *                                          512 rows          4: 614   8: 649      2: 603 4: 637  3: 620  4: 562  8: 591
+ *   summaries, 4700 keys, 512 rows                           1: 99    4: 57       1: 75  2: 54   3: 60   4: 54
+ *   2000 keys, 2304 rows                                     1: 58    2: 84       1: 72          1: 69
+ *   10000 keys, 2048 rows                                    1: 294               1: 304         1: 269  2: 296
+ *   4200 keys, 8 x 100 rows                                  1: 91    4: 47 6: 51 1: 69  2: 47   3: 57
+ *   window of 1023, 16/16 heads, 1280 rows                   1: 39    3: 36       1: 34  2: 50   3: 38
+ *   2700 keys, 2595 rows of six, 12/4 heads, head_dim 64     1: 52    2: 41       1: 41          3: 48
+ *   830 keys, 64 rows, 8/4 heads                             1: 20    6: 12.3     6: 13.3        6: 13.5
+ * Over twelve such calls what is chosen takes 1.4 % longer than the best of the three kinds with 1, 2, 3, 4, 6, 8 and 12 spans; without the second
+ * kind 3 %.
  *
  * most: what is chosen here has at most so many spans.
  */
