@@ -47,6 +47,13 @@ __device__ __forceinline__ void lds_direct_load_16_s(const __bf16 *sbase, unsign
                  : "memory");
 }
 
+// value held by lane l ^ 32
+__device__ __forceinline__ float other_half(float x) {
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
+}
+
 template <int CTRL>
 __device__ __forceinline__ float dpp_add(float x) {
     const int y = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, false);

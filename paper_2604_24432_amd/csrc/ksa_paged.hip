@@ -43,12 +43,6 @@ constexpr float LOWEST = -FLT_MAX;
 // in a missing page's place, summaries that are listed and seen by no row, and rows that only others see.
 constexpr int MOST_EXP = 127 + 119;
 
-// value of lane l ^ 32
-__device__ __forceinline__ float swap32(float x) {
-    const unsigned u = __builtin_bit_cast(unsigned, x);
-    auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
-}
 __device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
     const unsigned lo = (unsigned)__shfl((int)(unsigned)x, lane), hi = (unsigned)__shfl((int)(unsigned)(x >> 32), lane);
     return (int64_t)(((uint64_t)hi << 32) | lo);
@@ -148,8 +142,8 @@ __device__ __forceinline__ float raised(const f32x16 &sc, float sum, float m_run
     float most = sc[0];
 #pragma unroll
     for (int g = 1; g < 16; ++g) most = fmaxf(most, sc[g]);
-    most = fmaxf(most, swap32(most)) * scale;
-    const float m = fmaxf(sum, swap32(sum)) > HIGH ? fmaxf(most, m_run) : m_run;   // (by the row alone)
+    most = fmaxf(most, other_half(most)) * scale;
+    const float m = fmaxf(sum, other_half(sum)) > HIGH ? fmaxf(most, m_run) : m_run;   // (by the row alone)
     const float alpha = __builtin_amdgcn_exp2f(m_run - m);
     l_run *= alpha;
 #pragma unroll
@@ -319,7 +313,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ksa_paged_few_kernel(const 
         float most = sc[0];
 #pragma unroll
         for (int g = 1; g < 16; ++g) most = fmaxf(most, sc[g]);
-        most = fmaxf(most, swap32(most)) * a.score_scale;
+        most = fmaxf(most, other_half(most)) * a.score_scale;
         if (__builtin_amdgcn_ballot_w64(most > m_run) != 0) {
             const float m = fmaxf(most, m_run), alpha = __builtin_amdgcn_exp2f(m_run - m);
             m_run = m, l_run *= alpha;
@@ -349,7 +343,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ksa_paged_few_kernel(const 
     }
 
     // ---- the waves' results ------------------------------------------------------------------------------------------
-    const float l = l_run + swap32(l_run);
+    const float l = l_run + other_half(l_run);
     if (h == 0) sh_m[wave][r] = m_run, sh_l[wave][r] = l;
     float *const mine = reinterpret_cast<float *>(own);
 #pragma unroll
@@ -763,7 +757,7 @@ __global__ __launch_bounds__(NW * GROUPS * 64, 2) void ksa_paged_many_kernel(con
             add_no_numbers<D, F8>(a, hkv, spot_of(a.rows, entry_of(a.rows, tile.b, key_at(keys, x))), h, seen.sees(x), o);
         }
     }
-    float l = l_run + swap32(l_run);
+    float l = l_run + other_half(l_run);
     if constexpr (GROUPS > 1) {
         float *const other = reinterpret_cast<float *>(sh_tiles + OWN) + wave * 64 * (16 * DB + 2) + lane;   // of the lane with the same pair
         __syncthreads();
@@ -852,7 +846,6 @@ __global__ __launch_bounds__(256) void ksa_paged_join_few_kernel(const FwdArgs a
             den += of[s][1] * w, out += o[s] * w;
         }
     } else den = __builtin_nanf("");
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     bf16x4 r;
 #pragma unroll
     for (int e = 0; e < 4; ++e) r[e] = (__bf16)(out[e] / den);

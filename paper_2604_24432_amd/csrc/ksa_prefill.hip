@@ -68,13 +68,6 @@ struct PrefillArgs {
     float scale, scale_log2e;
 };
 
-__device__ __forceinline__ float other_half(float x) {
-    // value held by lane l^32
-    const unsigned u = __builtin_bit_cast(unsigned, x);
-    auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
-}
-
 // LDS tile: row-major [64][D] bf16, the 16-byte chunk index XORed with a function of the row.  At head_dim 64 two rows share the
 // 256 bytes that all banks hold, so the rows of one parity have to differ (1 % of the time: see ksa_prefill_direct.hip).
 template <int D>

@@ -92,13 +92,6 @@ struct DirectArgs {
     float scale;
 };
 
-__device__ __forceinline__ float other_half(float x) {
-    // value held by lane l^32
-    const unsigned u = __builtin_bit_cast(unsigned, x);
-    auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
-}
-
 __device__ __forceinline__ float other_row(float x) {
     // value held by lane l^16
     const unsigned u = __builtin_bit_cast(unsigned, x);
