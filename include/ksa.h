@@ -362,7 +362,8 @@ typedef struct ksa_paged_cache {
  * spans; what ksa_params excludes), HIP.
  */
 
-/* Columns that the tables need for the first n_rows augmented rows of a sequence. */
+/* Columns that the tables need for the first n_rows augmented rows of a sequence.  Errors: INVALID_ARG, OUT_OF_RANGE (n_rows beyond the rows of
+ * params->n_text text tokens). */
 int ksa_paged_pages(const ksa_params *params /*host*/, int32_t page_rows, int64_t n_rows, int64_t *text_pages /*host*/,
                     int64_t *summary_pages /*host*/);
 

@@ -23,3 +23,33 @@ def test_chunks_longer_than_any_text(c, m, rows):
     plain = K.make_params(1, 100, 1, 0, 200, 4, 2, 64)     # the same rows and keys, as a window longer than the text
     want, want_lse, off, lse_off = attend(q.double(), k.double(), v.double(), list(range(100 - rows, 100)), plain)
     assert bool(((o.double() - want).abs() <= off).all()) and bool(((lse.double() - want_lse).abs() <= lse_off).all())
+
+
+# heads, KV heads, d, text tokens to reckon with, rows of two sequences, spans: every kernel, every way of joining spans
+CALLS = [(32, 8, 128, 8192, (1, 1), 0), (8, 1, 64, 8192, (3, 2), 5), (32, 8, 128, 8192, (2, 1), 2), (16, 2, 64, 2048, (65, 40), 1), (16, 2, 128, 2048, (300, 1), 3),
+         (4, 2, 64, 16384, (300, 20), 1), (4, 2, 128, 16384, (300, 20), 9), (64, 2, 64, 16384, (1100, 900), 1), (64, 2, 128, 16384, (1100, 900), 4)]
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("case", CALLS, ids=str)
+def test_the_same_call_gives_the_same_bits(case, fp8):
+    Hq, Hkv, d, n_text, rows, n_splits = case
+    print(f"paged repeated calls {case} fp8={fp8}", flush=True)
+    p = K.make_params(2, n_text, 16, 2, 2, Hq, Hkv, d)
+    L = [1700, 1233]
+    pages = Pages(p, L, 16, fp8, 5)
+    for b in range(2):
+        pages.put(b, 0, randn(L[b], Hkv, d, seed=b), randn(L[b], Hkv, d, seed=b + 5))
+    q = randn(sum(rows), Hq, d, seed=9)
+    cu, start = batch_of([n - r for n, r in zip(L, rows)], rows)
+    o0, lse0 = K.ksa_paged_fwd(pages.cache, q, cu, start, max_rows=max(rows), n_splits=n_splits)
+    for turn in range(6):
+        if turn % 2:      # something else on the chip meanwhile, in front of the call and beside it
+            other = torch.cuda.Stream()
+            with torch.cuda.stream(other):
+                x = torch.randn(1024, 1024, device="cuda")
+                for _ in range(4):
+                    x = x @ x * 1e-3
+        o, lse = K.ksa_paged_fwd(pages.cache, q, cu, start, max_rows=max(rows), n_splits=n_splits)
+        assert torch.equal(o.view(torch.int16), o0.view(torch.int16)) and torch.equal(lse, lse0)
+        torch.cuda.synchronize()
