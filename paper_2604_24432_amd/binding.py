@@ -699,7 +699,7 @@ def ksa_paged_fwd(cache: PagedCache, q, cu_rows, start, max_rows: Optional[int] 
                   n_splits: int = 0, stream=None):
     """q [rows, Hq, d] bf16, the queries of the rows that ksa_paged_append wrote -> o like q, lse [rows, Hq] fp32; no gradients.
     max_rows: the largest number of rows of a sequence; omitted it is all of them, with which single rows of several sequences take the kernel for
-    many rows (64 sequences 1.2 to 1.9 times as long); workspace: uint8, at least
+    many rows (64 sequences 1.2 to 2.3 times as long); workspace: uint8, at least
     paged_workspace_bytes(cache, rows, max_rows, n_splits) bytes (allocated here if omitted; with n_splits = 0 a smaller one, of any size, means
     fewer spans).  What is allocated here belongs to `stream`."""
     import torch
