@@ -314,7 +314,7 @@ int ksa_decode_summary_fwd(const ksa_params *params /*host*/, const void *q, con
                            const int64_t cache_strides[3], void *workspace, size_t workspace_bytes,
                            int32_t n_splits, void *stream);
 
-/* ---- paged cache: many new rows per sequence, bf16 or 8-bit floats ------------------------------------------- */
+/* ---- paged cache: many new rows per sequence, bf16, 8-bit or 4-bit floats ------------------------------------------- */
 
 /*
  * A batch of augmented sequences (Eq. 1) whose K / V rows lie in pages of one pool.  A page is page_rows rows of every KV
@@ -331,9 +331,16 @@ int ksa_decode_summary_fwd(const ksa_params *params /*host*/, const void *q, con
  * NaN.  k_exp and v_exp hold e + 127.  With a byte there that is none of those (in a slot never written) the rows that see it may come out as
  * anything, and only they.  What a row stands for is zero or a normal bf16 number per element: reading it back and attending to it
  * add no rounding.
+ *
+ * KSA_CACHE_FP4 holds a row of one KV head in groups of 32 elements, each as 4-bit floats (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) times
+ * a power of two 2^e of the group's: e is the least integer in [-125, 125] with max |x| <= 7 * 2^e over the group (7, half way to the 8 that e2m1 lacks, and
+ * what lies beyond become 6), every element is x / 2^e rounded to the nearest e2m1 number (ties to the even code).  Two elements are a byte, the one
+ * with the even index in the low bits.  k_exp and v_exp hold e + 127 per group; 255 says that some element of the group was an infinity or NaN: then all
+ * 32 are NaN.  Other bytes (in a slot never written) are as above.  Here too reading and attending add no rounding.
  */
 #define KSA_CACHE_BF16 0
 #define KSA_CACHE_FP8 1
+#define KSA_CACHE_FP4 2
 typedef struct ksa_paged_cache {
     int32_t format;                 /* KSA_CACHE_*                                                                     */
     int32_t page_rows;              /* rows per page: a power of two in [8, 1024]                                      */
@@ -343,9 +350,10 @@ typedef struct ksa_paged_cache {
     int32_t reserved;               /* 0                                                                               */
     const int32_t *text_table;      /* device [batch, text_pages]                                                      */
     const int32_t *summary_table;   /* device [batch, summary_pages]; may be NULL if n_summary is 0                    */
-    void *k, *v;                    /* device, bf16 or e4m3, [n_pages, Hkv, page_rows, d], last dim contiguous         */
-    uint8_t *k_exp, *v_exp;         /* device [n_pages, Hkv, page_rows] contiguous for KSA_CACHE_FP8, else NULL        */
-    int64_t strides[3];             /* of k and v: {page, head, row} in elements, multiples of 16 bytes; {0, 0, 0} = contiguous */
+    void *k, *v;                    /* device, bf16, e4m3 or pairs of e2m1, [n_pages, Hkv, page_rows, d (pairs: d / 2)], last dim contiguous */
+    uint8_t *k_exp, *v_exp;         /* device, contiguous: [n_pages, Hkv, page_rows] for KSA_CACHE_FP8, [n_pages, Hkv, page_rows, d / 32] (on 4 bytes)
+                                       for KSA_CACHE_FP4, else NULL */
+    int64_t strides[3];             /* of k and v: {page, head, row} in elements (KSA_CACHE_FP4: bytes), multiples of 16 bytes; {0, 0, 0} = contiguous */
 } ksa_paged_cache;
 
 /*
@@ -403,6 +411,89 @@ size_t ksa_paged_workspace_bytes(const ksa_params *params /*host*/, int64_t tota
 int ksa_paged_fwd(const ksa_params *params /*host*/, const ksa_paged_cache *cache /*host*/, const void *q, void *o, float *lse,
                   const int64_t q_strides[2], const int64_t o_strides[2], const int32_t *cu_rows, const int32_t *start,
                   int64_t total_rows, int64_t max_rows, void *workspace, size_t workspace_bytes, int32_t n_splits, void *stream);
+
+/* ---- rotary positions ---------------------------------------------------------------------------------------------------- */
+
+/*
+ * Rotary positions turn pairs of a head's elements: (a, b) becomes magnitude * (a cos x - b sin x, b cos x + a sin x), x = position * f_i for pair i of dim / 2.
+ * The pairs are (2i, 2i + 1) with `interleaved`, else (i, i + dim / 2); elements from `dim` on stay as they are.  A text row's position is its text
+ * index, a summary row's that of its chunk's last text row (section 2.2.1, as ksa_layout_index_maps).  The caches take keys that have been turned.
+ * Frequencies are in turns per position, as fractions of 2^64, so that the angle of any position is exact to 2^-32 of a turn.
+ */
+typedef struct ksa_rotary {
+    int32_t dim;                    /* even, 2 .. head_dim                                    */
+    int32_t interleaved;            /* 0 or 1                                                 */
+    float magnitude;                /* finite, positive                                       */
+    int32_t reserved;               /* 0                                                      */
+    const uint64_t *turns;          /* device [dim / 2], 8-byte aligned (ksa_rotary_turns)    */
+} ksa_rotary;
+
+#define KSA_ROTARY_PLAIN 0          /* f_i = base^(-2i / dim) radians per position                                               */
+#define KSA_ROTARY_LINEAR 1         /* f_i / factor                                                                             */
+#define KSA_ROTARY_BY_PARTS 2       /* with r = original * f_i / 2 pi turns over the original context and s = (r - slow) / (fast - slow) kept within 0 .. 1:
+                                       f_i (s + (1 - s) / factor); magnitude 0.1 ln(factor) + 1                                  */
+typedef struct ksa_rotary_rule {
+    int32_t dim, scaling;           /* scaling: KSA_ROTARY_*                                                                    */
+    double base;                    /* more than 1                                                                              */
+    double factor;                  /* at least 1; by how much the context has grown                                             */
+    double original;                /* by parts: positions of the original context, more than 0                                 */
+    double slow, fast;              /* by parts: 0 <= slow < fast                                                               */
+} ksa_rotary_rule;
+
+/* The frequencies of a rule (host array [dim / 2]) and its magnitude (host), for a ksa_rotary.  Errors: INVALID_ARG. */
+int ksa_rotary_turns(const ksa_rotary_rule *rule /*host*/, uint64_t *turns /*host*/, float *magnitude /*host*/);
+
+/*
+ * ksa_rotary_fwd: rows of whole augmented sequences (those of params->n_text text tokens) are turned: q [B, L, Hq, d] into q_out, k [B, L, Hkv, d] into k_out,
+ * device bf16, last dim contiguous.  q and q_out, or k and k_out, may be NULL.  An output may be the memory of its input (same strides).
+ * *_strides = {batch, row, head} in elements, multiples of 8, positive; NULL = contiguous.  Angles and products are fp32, each output is rounded once.
+ * ksa_rotary_bwd: gradients with respect to q and k from those with respect to what ksa_rotary_fwd gave: turned back, times magnitude.
+ * Errors: INVALID_ARG (null or misaligned pointers: 16 bytes; bad strides or rotary fields), UNSUPPORTED (2^26 rows of all sequences and more), HIP.
+ */
+int ksa_rotary_fwd(const ksa_params *params /*host*/, const ksa_rotary *rotary /*host*/, const void *q, const void *k, void *q_out, void *k_out,
+                   const int64_t q_strides[3], const int64_t k_strides[3], const int64_t q_out_strides[3], const int64_t k_out_strides[3], void *stream);
+int ksa_rotary_bwd(const ksa_params *params /*host*/, const ksa_rotary *rotary /*host*/, const void *dq_out, const void *dk_out, void *dq, void *dk,
+                   const int64_t dq_out_strides[3], const int64_t dk_out_strides[3], const int64_t dq_strides[3], const int64_t dk_strides[3], void *stream);
+
+/*
+ * ksa_paged_rotary: a serving step's new rows in one launch: q (device bf16 [total_rows, Hq, d]) is turned into q_out, k_new is turned, and goes with v_new into the
+ * cache, as ksa_paged_append puts it (k is rounded to bf16 in between: the same bits as in two steps).  Batch, tables, capacity and errors as there (and UNSUPPORTED
+ * from 2^26 rows on); rows of q of a sequence out of place become NaN in q_out.  q and q_out may be NULL; q_out may be the memory of q (same strides).
+ */
+int ksa_paged_rotary(const ksa_params *params /*host*/, const ksa_paged_cache *cache /*host*/, const ksa_rotary *rotary /*host*/, const void *q, void *q_out,
+                     const void *k_new, const void *v_new, const int64_t q_strides[2], const int64_t q_out_strides[2], const int64_t kv_strides[2],
+                     const int32_t *cu_rows, const int32_t *start, int64_t total_rows, void *stream);
+
+/* ---- a step's rows and pages from the sequences' lengths --------------------------------------------------------------------- */
+
+/*
+ * ksa_paged_advance: what a step needs to know and to have, worked out on the device.  Sequence b holds held[b] text tokens (with the summaries of their
+ * whole chunks) and gets new_text[b] more, whose rows (text, and the summaries of every chunk that they complete) are the step's new rows: start[b] and
+ * cu_rows as the calls above take them.  new_text[b] < 0: the sequence has ended; it has no rows and gives all its pages back.  A sequence with held[b] < 0 or
+ * held[b] + new_text[b] > params->n_text is out of place: start[b] = -1, it has no rows and its pages stay.
+ *
+ * Pages: page_refs (device int32 [n_pages]) counts how many table entries name a page (a shared prompt: several); a page with 0 is free.  The call
+ *   - gives back (entry = -1, its page's count one less) text columns that only hold text which no row sees any more (Eq. 3 for a sequence that holds held[b]),
+ *     and the columns of sequences that have ended,
+ *   - gives a free page (entry = page, count 1) to every column that begins with or behind the first new row of its kind, holds a new row and has no page
+ *     (an entry outside [0, n_pages)): the lowest free pages, in the order of sequences, text before summaries, columns ascending,
+ * and leaves everything else, so a second call with the same lengths changes nothing.  A page must not take new rows while several entries name it: share whole pages.
+ * *lacking is the number of columns that got no page because none was free; their rows are not stored and read as NaN until the sequence ends.
+ * The cache's tables are written; k, v and the exponents are not looked at.
+ *
+ *   held, new_text: device int32 [batch]; cu_rows: device int32 [batch + 1]; start: device int32 [batch]; lacking: device int32 [1].
+ *   Row maps of the step's rows, device [total_rows], each may be NULL: slots (int64): page * page_rows + slot, -1 without a page; positions (int32): as rotary
+ *   positions take them; tokens (int32): the row's place among the new text tokens of all sequences, or -1 - s for the s-th summary of its chunk.  Rows behind the last
+ *   sequence's get -1, 0 and -1.  total_rows may be less than the rows there are; it only says how long the maps are.
+ *   workspace: device, 16-byte aligned, at least ksa_paged_advance_workspace_bytes bytes, needed until the work enqueued on `stream` has finished.
+ * Counts beyond 2^31 - 1 (cu_rows) stay there.  Nothing is allocated, cleared or waited for; the call may be captured into a graph.  Results do not depend on the
+ * order of execution.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^31 columns of
+ * both tables over all sequences, or rows, and more), HIP.
+ */
+size_t ksa_paged_advance_workspace_bytes(const ksa_params *params /*host*/, const ksa_paged_cache *cache /*host*/);
+int ksa_paged_advance(const ksa_params *params /*host*/, const ksa_paged_cache *cache /*host*/, int32_t *page_refs, const int32_t *held, const int32_t *new_text,
+                      int32_t *cu_rows, int32_t *start, int32_t *lacking, int64_t *slots, int32_t *positions, int32_t *tokens, int64_t total_rows,
+                      void *workspace, size_t workspace_bytes, void *stream);
 
 const char *ksa_status_string(int status);
 /* Static description of the build: tile sizes and the gfx target, e.g. for logs. */

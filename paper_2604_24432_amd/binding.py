@@ -10,7 +10,7 @@ import ctypes as C
 import os
 import struct
 from dataclasses import dataclass
-from typing import Optional, Tuple
+from typing import Any, NamedTuple, Optional, Tuple
 
 import numpy as np
 
@@ -41,6 +41,15 @@ def make_params(batch, n_text, chunk_len, n_summary, window_chunks, n_q_heads, n
         compress_ratio = chunk_len // n_summary if n_summary else 0
     return ksa_params(batch, n_text, chunk_len, n_summary, compress_ratio, window_chunks, n_q_heads,
                       n_kv_heads, head_dim, softmax_scale, flags)
+
+
+class ksa_rotary(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float), ("reserved", C.c_int32), ("turns", C.c_void_p)]
+
+
+class ksa_rotary_rule(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double), ("factor", C.c_double), ("original", C.c_double), ("slow", C.c_double),
+                ("fast", C.c_double)]
 
 
 _lib = None
@@ -90,6 +99,12 @@ def lib():
         "ksa_paged_read": (C.c_int, [pp, vp, vp, vp, i64p, vp, vp, C.c_int64, vp]),
         "ksa_paged_workspace_bytes": (C.c_size_t, [pp, C.c_int64, C.c_int64, C.c_int32]),
         "ksa_paged_fwd": (C.c_int, [pp, vp, vp, vp, vp, i64p, i64p, vp, vp, C.c_int64, C.c_int64, vp, C.c_size_t, C.c_int32, vp]),
+        "ksa_paged_advance_workspace_bytes": (C.c_size_t, [pp, vp]),
+        "ksa_paged_advance": (C.c_int, [pp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_int64, vp, C.c_size_t, vp]),
+        "ksa_rotary_turns": (C.c_int, [C.POINTER(ksa_rotary_rule), C.POINTER(C.c_uint64), C.POINTER(C.c_float)]),
+        "ksa_rotary_fwd": (C.c_int, [pp, vp, vp, vp, vp, vp, i64p, i64p, i64p, i64p, vp]),
+        "ksa_rotary_bwd": (C.c_int, [pp, vp, vp, vp, vp, vp, i64p, i64p, i64p, i64p, vp]),
+        "ksa_paged_rotary": (C.c_int, [pp, vp, vp, vp, vp, vp, vp, i64p, i64p, i64p, vp, vp, C.c_int64, vp]),
         "ksa_status_string": (C.c_char_p, [C.c_int]),
         "ksa_build_info": (C.c_char_p, []),
     }
@@ -107,7 +122,7 @@ EXPORTED_SYMBOLS = ("ksa_augmented_rows", "ksa_build_layout", "ksa_layout_destro
                     "ksa_cache_summary_row", "ksa_decode_ranges", "ksa_decode_workspace_bytes",
                     "ksa_decode_fwd", "ksa_decode_fwd_static", "ksa_decode_summary_ranges", "ksa_decode_summary_fwd", "ksa_cache_from_prefill",
                     "ksa_cache_append", "ksa_paged_pages", "ksa_paged_append", "ksa_paged_read", "ksa_paged_workspace_bytes", "ksa_paged_fwd",
-                    "ksa_status_string", "ksa_build_info")
+                    "ksa_paged_advance_workspace_bytes", "ksa_paged_advance", "ksa_rotary_turns", "ksa_rotary_fwd", "ksa_rotary_bwd", "ksa_paged_rotary", "ksa_status_string", "ksa_build_info")
 
 
 def status_string(status: int) -> str:
@@ -528,7 +543,7 @@ def _append_checks(params: ksa_params, k_new, v_new, pos, k_cache, v_cache):
     return _strides3(k_cache)
 
 
-KSA_CACHE_BF16, KSA_CACHE_FP8 = 0, 1
+KSA_CACHE_BF16, KSA_CACHE_FP8, KSA_CACHE_FP4 = 0, 1, 2
 
 
 class ksa_paged_cache(C.Structure):
@@ -540,7 +555,8 @@ class ksa_paged_cache(C.Structure):
 class PagedCache:
     """A batch of sequences whose K / V rows lie in the pages of one pool (struct ksa_paged_cache); holds its tensors.
 
-    k, v: [n_pages, Hkv, page_rows, d] on the GPU, bfloat16, or float8_e4m3fn with k_exp, v_exp uint8 [n_pages, Hkv, page_rows].
+    k, v: [n_pages, Hkv, page_rows, d] on the GPU, bfloat16, or float8_e4m3fn with k_exp, v_exp uint8 [n_pages, Hkv, page_rows], or 4-bit floats, two to a
+    byte: uint8 [n_pages, Hkv, page_rows, d / 2] with k_exp, v_exp uint8 [n_pages, Hkv, page_rows, d / 32].
     text_table, summary_table: int32 [batch, columns], contiguous; their contents may change from call to call.  Other tensors, or other
     parameters, take another PagedCache.  A cache carries no gradient: what is appended, read or attended to is not recorded for autograd.
     """
@@ -548,18 +564,19 @@ class PagedCache:
     def __init__(self, params: ksa_params, k, v, text_table, summary_table=None, k_exp=None, v_exp=None):
         import torch
         params = ksa_params.from_buffer_copy(params)
-        f8 = k.dtype is torch.float8_e4m3fn
+        f8, f4 = k.dtype is torch.float8_e4m3fn, k.dtype is torch.uint8
         for t, name in ((k, "k"), (v, "v")):
-            _require(t, name, torch.float8_e4m3fn if f8 else torch.bfloat16, 4)
+            _require(t, name, torch.float8_e4m3fn if f8 else torch.uint8 if f4 else torch.bfloat16, 4)
         n_pages, heads, rows, d = k.shape
-        if (heads, d) != (params.n_kv_heads, params.head_dim) or k.shape != v.shape or not _same_strides(k, v):
-            raise ValueError(f"k / v shape must be [n_pages, {params.n_kv_heads}, page_rows, {params.head_dim}], with the same strides")
-        if f8 != (k_exp is not None) or f8 != (v_exp is not None):
-            raise ValueError("k_exp and v_exp belong to a float8_e4m3fn cache, and to no other")
-        for t, name in ((k_exp, "k_exp"), (v_exp, "v_exp")) if f8 else ():
-            _require(t, name, torch.uint8, 3)
-            if tuple(t.shape) != (n_pages, heads, rows) or not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous {(n_pages, heads, rows)}")
+        if (heads, d) != (params.n_kv_heads, params.head_dim // 2 if f4 else params.head_dim) or k.shape != v.shape or not _same_strides(k, v):
+            raise ValueError(f"k / v shape must be [n_pages, {params.n_kv_heads}, page_rows, {params.head_dim}{' / 2' if f4 else ''}], with the same strides")
+        if (f8 or f4) != (k_exp is not None) or (f8 or f4) != (v_exp is not None):
+            raise ValueError("k_exp and v_exp belong to a float8_e4m3fn or 4-bit (uint8) cache, and to no other")
+        exps = (n_pages, heads, rows, params.head_dim // 32) if f4 else (n_pages, heads, rows)
+        for t, name in ((k_exp, "k_exp"), (v_exp, "v_exp")) if f8 or f4 else ():
+            _require(t, name, torch.uint8, len(exps))
+            if tuple(t.shape) != exps or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous {exps}")
         if params.n_summary > 0 and summary_table is None:
             raise ValueError("summary_table is missing")
         for t, name in ((text_table, "text_table"), (summary_table, "summary_table")):
@@ -573,7 +590,7 @@ class PagedCache:
         self.params, self.device = params, k.device
         self.k, self.v, self.text_table, self.summary_table, self.k_exp, self.v_exp = k, v, text_table, summary_table, k_exp, v_exp
         ptr = [t.data_ptr() if t is not None else None for t in (text_table, summary_table, k, v, k_exp, v_exp)]
-        self.struct = ksa_paged_cache(KSA_CACHE_FP8 if f8 else KSA_CACHE_BF16, rows, n_pages, text_table.shape[1],
+        self.struct = ksa_paged_cache(KSA_CACHE_FP8 if f8 else KSA_CACHE_FP4 if f4 else KSA_CACHE_BF16, rows, n_pages, text_table.shape[1],
                                       summary_table.shape[1] if summary_table is not None else 0, 0, *ptr, _strides_of(k))
 
         # what a call needs of all this, as it needs it
@@ -730,6 +747,198 @@ def ksa_paged_fwd(cache: PagedCache, q, cu_rows, start, max_rows: Optional[int] 
     _paged(cache, "ksa_paged_fwd", stream, q.data_ptr(), o.data_ptr(), lse.data_ptr() if lse is not None else None, q_strides, o_strides,
            cu_rows.data_ptr(), start.data_ptr(), rows, max_rows, workspace.data_ptr(), workspace.numel(), n_splits)
     return o, lse
+
+
+# ---- rotary positions --------------------------------------------------------------------------------
+
+KSA_ROTARY_PLAIN, KSA_ROTARY_LINEAR, KSA_ROTARY_BY_PARTS = 0, 1, 2
+_SCALINGS = {None: KSA_ROTARY_PLAIN, "linear": KSA_ROTARY_LINEAR, "by_parts": KSA_ROTARY_BY_PARTS}
+
+
+def rotary_turns(dim: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0, original: float = 1.0, slow: float = 1.0,
+                 fast: float = 32.0) -> Tuple[np.ndarray, float]:
+    """The frequencies of a rule, uint64 [dim / 2] in turns per position times 2^64, and its magnitude (struct ksa_rotary_rule)."""
+    if scaling not in _SCALINGS:
+        raise ValueError(f"scaling must be one of {tuple(_SCALINGS)}")
+    turns, magnitude = np.zeros(max(dim // 2, 1), np.uint64), C.c_float()
+    rule = ksa_rotary_rule(dim, _SCALINGS[scaling], base, factor, original, slow, fast)
+    _check(lib().ksa_rotary_turns(C.byref(rule), turns.ctypes.data_as(C.POINTER(C.c_uint64)), C.byref(magnitude)), "ksa_rotary_turns")
+    return turns, magnitude.value
+
+
+class Rotary:
+    """Rotary positions (struct ksa_rotary): the first `dim` elements of a head are turned in pairs, (2i, 2i + 1) if interleaved, else (i, i + dim / 2), by
+    position * base^(-2i / dim).  scaling: None; "linear" (all frequencies divided by factor); "by_parts" (those that turn less than `slow` times
+    over `original` positions are, those that turn more than `fast` times are not, between them in proportion).  magnitude scales what is turned; None: 1, by
+    parts 0.1 ln(factor) + 1.  Holds the frequencies on the device."""
+
+    def __init__(self, dim: int, base: float = 10000.0, interleaved: bool = False, scaling: Optional[str] = None, factor: float = 1.0, original: float = 1.0,
+                 slow: float = 1.0, fast: float = 32.0, magnitude: Optional[float] = None, device="cuda"):
+        import torch
+        turns, by_rule = rotary_turns(dim, base, scaling, factor, original, slow, fast)
+        self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
+        if not self.turns.is_cuda:
+            raise ValueError("device must be a GPU")
+        self.device, self._dev = self.turns.device, self.turns.device.index
+        self.struct = ksa_rotary(dim, 1 if interleaved else 0, by_rule if magnitude is None else magnitude, 0, self.turns.data_ptr())
+        self._arg = C.byref(self.struct)
+
+    @property
+    def dim(self) -> int:
+        return self.struct.dim
+
+
+def _on_device(dev, name, stream, *args):
+    """The call on device `dev`: on `stream`, or on that device's current one."""
+    from torch import _C
+    here = _C._cuda_getDevice()
+    if stream is None:
+        raw = _C._cuda_getCurrentRawStream(dev)
+    elif stream.device.index != dev:
+        raise ValueError("stream belongs to another device than the tensors")
+    else:
+        raw = stream.cuda_stream
+    if here == dev:
+        rc = getattr(lib(), name)(*args, raw)
+    else:
+        _C._cuda_setDevice(dev)
+        try:
+            rc = getattr(lib(), name)(*args, raw)
+        finally:
+            _C._cuda_setDevice(here)
+    if rc:
+        _check(rc, name)
+
+
+def _rotary_call(name, params: ksa_params, rotary: Rotary, tensors, outputs, names, stream):
+    import torch
+    if tensors[0] is None and tensors[1] is None:
+        raise ValueError(f"{names[0]} and {names[1]} are both missing")
+    if stream is not None and any(x is not None and y is None for x, y in zip(tensors, outputs)):
+        if stream.device != rotary.device:
+            raise ValueError("stream belongs to another device than the tensors")
+        with torch.cuda.stream(stream):      # what is allocated here belongs to `stream`
+            return _rotary_call(name, params, rotary, tensors, outputs, names, None)
+    rows = augmented_rows(params, params.n_text)
+    out, ptr, strides = [], [], []
+    for x, y, what, heads in zip(tensors, outputs, names, (params.n_q_heads, params.n_kv_heads)):
+        if x is None:
+            if y is not None:
+                raise ValueError(f"an output is given for {what}, which is missing")
+            out.append(None), ptr.append((None, None)), strides.append((None, None))
+            continue
+        y = torch.empty_like(x) if y is None else y
+        for t in (x, y):
+            _require(t, what, torch.bfloat16, 4)
+            if tuple(t.shape) != (params.batch, rows, heads, params.head_dim):
+                raise ValueError(f"{what}: expected {(params.batch, rows, heads, params.head_dim)}, got {tuple(t.shape)}")
+            if t.get_device() != rotary._dev:
+                raise ValueError(f"{what} lies on another device than the frequencies")
+        out.append(y), ptr.append((x.data_ptr(), y.data_ptr())), strides.append((_strides_of(x), _strides_of(y)))
+    (q, q_out), (k, k_out) = ptr
+    _on_device(rotary._dev, name, stream, C.byref(params), rotary._arg, q, k, q_out, k_out, strides[0][0], strides[1][0], strides[0][1], strides[1][1])
+    return tuple(out)
+
+
+def ksa_rotary_fwd(params: ksa_params, rotary: Rotary, q, k, q_out=None, k_out=None, stream=None):
+    """q [B, L, Hq, d], k [B, L, Hkv, d] bf16 of whole augmented sequences -> both turned by their rows' positions (a summary row's is that of its chunk's last
+    text).  q or k may be None; an output may be its input.  Gradients: ksa_rotary_bwd."""
+    return _rotary_call("ksa_rotary_fwd", params, rotary, (q, k), (q_out, k_out), ("q", "k"), stream)
+
+
+def ksa_rotary_bwd(params: ksa_params, rotary: Rotary, dq_out, dk_out, dq=None, dk=None, stream=None):
+    """Gradients with respect to ksa_rotary_fwd's outputs -> with respect to its q and k."""
+    return _rotary_call("ksa_rotary_bwd", params, rotary, (dq_out, dk_out), (dq, dk), ("dq_out", "dk_out"), stream)
+
+
+def ksa_paged_rotary(cache: PagedCache, rotary: Rotary, q, k_new, v_new, cu_rows, start, q_out=None, stream=None):
+    """ksa_paged_append of the turned k_new and of v_new [rows, Hkv, d], and q [rows, Hq, d] turned -> q_out, in one launch.  q may be None; q_out may be q.
+    What is allocated here belongs to `stream`."""
+    import torch
+    if stream is not None and q is not None and q_out is None:
+        _check_stream(cache, stream)
+        with torch.cuda.stream(stream):
+            return ksa_paged_rotary(cache, rotary, q, k_new, v_new, cu_rows, start)
+    if rotary._dev != cache._dev:
+        raise ValueError("the frequencies lie on another device than the cache")
+    kv_strides = q_strides = out_strides = None
+    if not cache._plain(k_new, v_new, cache._kv, cu_rows, start):
+        _rows_of_call(cache, ((k_new, "k_new"), (v_new, "v_new")), cache.params.n_kv_heads, cu_rows, start)
+        if not _same_strides(k_new, v_new):
+            raise ValueError("k_new and v_new must have the same strides")
+        kv_strides = _strides_of(k_new)
+    if q is None:
+        if q_out is not None:
+            raise ValueError("q_out is given, q is missing")
+    else:
+        if q_out is None:
+            q_out = torch.empty_like(q)
+        if not cache._plain(q, q_out, cache._q, cu_rows, start):
+            _rows_of_call(cache, ((q, "q"), (q_out, "q_out")), cache.params.n_q_heads, cu_rows, start)
+            q_strides, out_strides = _strides_of(q), _strides_of(q_out)
+        if q.shape[0] != k_new.shape[0]:
+            raise ValueError("q must have as many rows as k_new")
+    _paged(cache, "ksa_paged_rotary", stream, rotary._arg, q.data_ptr() if q is not None else None, q_out.data_ptr() if q is not None else None, k_new.data_ptr(),
+           v_new.data_ptr(), q_strides, out_strides, kv_strides, cu_rows.data_ptr(), start.data_ptr(), k_new.shape[0])
+    return q_out
+
+
+# ---- a step's rows and pages ----------------------------------------------------------------------------
+
+
+class PagedStep(NamedTuple):
+    """What ksa_paged_advance works out, on the GPU."""
+    cu_rows: Any      # int32 [batch + 1]
+    start: Any        # int32 [batch]
+    lacking: Any      # int32 [1]: columns that got no page
+    slots: Any        # int64 [total_rows]: page * page_rows + slot, -1 without a page
+    positions: Any    # int32 [total_rows]: rotary positions
+    tokens: Any       # int32 [total_rows]: place among the new text tokens, or -1 - s for the s-th summary of its chunk
+
+
+def paged_advance_workspace_bytes(cache: PagedCache) -> int:
+    return int(lib().ksa_paged_advance_workspace_bytes(*cache._args))
+
+
+def _new_step(cache: PagedCache, total_rows: int) -> PagedStep:
+    import torch
+    batch = cache._batch[1][0]
+    i32 = lambda n: torch.empty(n, dtype=torch.int32, device=cache.device)  # noqa: E731
+    return PagedStep(i32(batch + 1), i32(batch), i32(1), torch.empty(total_rows, dtype=torch.int64, device=cache.device), i32(total_rows), i32(total_rows))
+
+
+def ksa_paged_advance(cache: PagedCache, page_refs, held, new_text, total_rows: int, step: Optional[PagedStep] = None, workspace=None, stream=None) -> PagedStep:
+    """held, new_text int32 [batch]: text tokens that every sequence holds, and that come (-1: it has ended) -> the step's rows (PagedStep; `step`, one of an
+    earlier call, is written again).  The cache's tables and page_refs (int32 [n_pages], table entries that name a page) are brought up to date: columns that nobody sees any
+    more are given back, new ones get the lowest free pages.  total_rows: length of the row maps; rows behind the last sequence's get -1, 0 and -1.
+    workspace: uint8, at least paged_advance_workspace_bytes(cache) bytes (allocated here if omitted).  What is allocated here belongs to `stream`."""
+    import torch
+    if stream is not None and (step is None or workspace is None):
+        _check_stream(cache, stream)
+        with torch.cuda.stream(stream):
+            return ksa_paged_advance(cache, page_refs, held, new_text, total_rows, step, workspace)
+    if total_rows < 0:
+        raise ValueError("total_rows must not be negative")
+    batch = cache._batch[1]
+    if step is None:
+        step = _new_step(cache, total_rows)
+        tensors = ((page_refs, "page_refs", (cache.struct.n_pages,)), (held, "held", batch), (new_text, "new_text", batch))
+    else:
+        rows = (total_rows,)
+        tensors = ((page_refs, "page_refs", (cache.struct.n_pages,)), (held, "held", batch), (new_text, "new_text", batch), (step.cu_rows, "cu_rows", cache._batch[0]),
+                   (step.start, "start", batch), (step.lacking, "lacking", (1,)), (step.positions, "positions", rows), (step.tokens, "tokens", rows))
+        if step.slots.dtype is not torch.int64 or step.slots.shape != rows or not step.slots.is_contiguous() or step.slots.get_device() != cache._dev:
+            raise ValueError(f"slots must be contiguous int64 {rows} on the cache's device")
+    for t, name, shape in tensors:
+        if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous() or t.get_device() != cache._dev:
+            raise ValueError(f"{name} must be contiguous int32 {tuple(shape)} on the cache's device")
+    if workspace is None:
+        workspace = torch.empty(paged_advance_workspace_bytes(cache), dtype=torch.uint8, device=cache.device)
+    elif workspace.dtype is not torch.uint8 or workspace.get_device() != cache._dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
+    _paged(cache, "ksa_paged_advance", stream, page_refs.data_ptr(), held.data_ptr(), new_text.data_ptr(), step.cu_rows.data_ptr(), step.start.data_ptr(),
+           step.lacking.data_ptr(), step.slots.data_ptr(), step.positions.data_ptr(), step.tokens.data_ptr(), total_rows, workspace.data_ptr(), workspace.numel())
+    return step
 
 
 def pack_cache(params: ksa_params, k_sum, v_sum, k_txt, v_txt, txt_base: int):

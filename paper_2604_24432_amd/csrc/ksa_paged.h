@@ -23,6 +23,31 @@ struct KsaPagedMove {
 };
 int ksa_launch_paged_append(const KsaPagedMove &a, void *stream);
 int ksa_launch_paged_read(const KsaPagedMove &a, void *stream);
+void ksa_launch_paged_append_fp4(const KsaPagedMove &a, void *stream);
+void ksa_launch_paged_read_fp4(const KsaPagedMove &a, void *stream);
+
+// ... turned on their way, and q with them (null: no q)
+struct KsaPagedRotary {
+    KsaPagedMove move;
+    ksa_rotary rotary;
+    const void *q;
+    void *q_out;
+    int64_t q_strides[2], out_strides[2];   // {row, head}
+};
+int ksa_launch_paged_rotary(const KsaPagedRotary &a, void *stream);
+
+// a step's rows and pages
+struct KsaPagedAdvance {
+    KsaPagedCall call;
+    int32_t *page_refs;
+    const int32_t *held, *new_text;
+    int32_t *cu_rows, *start, *lacking;
+    int64_t *slots;
+    int32_t *positions, *tokens;
+    int32_t *workspace;
+};
+size_t ksa_paged_advance_ints(int32_t batch, int32_t n_pages);   // of the workspace
+int ksa_launch_paged_advance(const KsaPagedAdvance &a, void *stream);
 
 #define KSA_PAGED_FEW 32
 // How the attention of a call is dealt to workgroups.
@@ -46,6 +71,7 @@ struct KsaPagedFwd {
     int32_t max_rows;
 };
 int ksa_launch_paged_fwd(const KsaPagedFwd &a, void *stream);
+void ksa_launch_paged_fwd_fp4(const KsaPagedFwd &a, void *stream);   // all but the join of spans
 
 #ifdef __HIPCC__
 #include "ksa_device.h"
@@ -98,6 +124,11 @@ __device__ __forceinline__ NewRows sequence_of(const PagedRows &a, int first, in
 __device__ __forceinline__ u32x2 unpack_fp8(unsigned x, float scale) {
     return {__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false)),
             __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true))};
+}
+// Eight e2m1 numbers times `scale`, a power of two (NaN where its exponent is 255), as bf16.
+__device__ __forceinline__ u32x4 unpack_fp4(unsigned x, float scale) {
+    return {__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 0)), __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 1)),
+            __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 2)), __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3))};
 }
 __device__ __forceinline__ float power_of_two(int biased) { return __builtin_bit_cast(float, biased << 23); }
 

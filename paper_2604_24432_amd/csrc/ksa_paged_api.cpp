@@ -2,65 +2,9 @@
 #include <algorithm>
 #include <cmath>
 
-#include "ksa_internal.h"
-#include "ksa_paged.h"
+#include "ksa_paged_checks.h"
 
 namespace {
-
-bool aligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-
-// augmented rows of a chunk; one that is longer than every text may exceed 32 bits
-int64_t chunk_rows(const ksa_params *p) { return (int64_t)p->chunk_len + p->n_summary; }
-int64_t augmented(const ksa_params *p) {
-    return (p->n_text / p->chunk_len) * chunk_rows(p) + p->n_text % p->chunk_len;
-}
-
-int check_sizes(const ksa_params *p, int64_t total_rows) {
-    const int rc = ksa_validate_params(p);
-    if (rc != KSA_OK) return rc;
-    if (total_rows < 0) return KSA_ERR_INVALID_ARG;
-    if (total_rows >= ((int64_t)1 << 31) / p->n_q_heads) return KSA_ERR_UNSUPPORTED;   // (row, head) pairs are int32 on the device
-    return KSA_OK;
-}
-
-// The cache and the batch of a call, checked, with defaults filled in.
-int check_call(KsaPagedCall &c, const ksa_params *p, const ksa_paged_cache *cache, const int32_t *cu_rows, const int32_t *start, int64_t total_rows) {
-    const int rc = check_sizes(p, total_rows);
-    if (rc != KSA_OK) return rc;
-    if (!cache || !cu_rows || !start || !aligned(cu_rows, 4) || !aligned(start, 4)) return KSA_ERR_INVALID_ARG;
-    const bool f8 = cache->format == KSA_CACHE_FP8;
-    if ((!f8 && cache->format != KSA_CACHE_BF16) || cache->reserved != 0) return KSA_ERR_INVALID_ARG;
-    const int32_t rows = cache->page_rows;
-    if (rows < 8 || rows > 1024 || (rows & (rows - 1)) || cache->n_pages <= 0) return KSA_ERR_INVALID_ARG;
-    if (cache->text_pages <= 0 || !cache->text_table || !aligned(cache->text_table, 4)) return KSA_ERR_INVALID_ARG;
-    if (p->n_summary > 0 && (cache->summary_pages <= 0 || !cache->summary_table)) return KSA_ERR_INVALID_ARG;
-    if (cache->summary_pages < 0 || !aligned(cache->summary_table, 4)) return KSA_ERR_INVALID_ARG;
-    if (!cache->k || !cache->v || !aligned(cache->k, 16) || !aligned(cache->v, 16)) return KSA_ERR_INVALID_ARG;
-    if (f8 != (cache->k_exp != nullptr) || f8 != (cache->v_exp != nullptr)) return KSA_ERR_INVALID_ARG;
-    const int64_t *s = cache->strides, size = f8 ? 1 : 2;
-    if (s[0] == 0 && s[1] == 0 && s[2] == 0) {
-        c.cache_strides[2] = p->head_dim * size;
-        c.cache_strides[1] = rows * c.cache_strides[2];
-        c.cache_strides[0] = p->n_kv_heads * c.cache_strides[1];
-    } else {
-        for (int x = 0; x < 3; ++x) {
-            if (s[x] <= 0 || s[x] > INT64_MAX / 2 || (s[x] * size) % 16 != 0) return KSA_ERR_INVALID_ARG;
-            c.cache_strides[x] = s[x] * size;
-        }
-    }
-    c.p = *p, c.cache = *cache;
-    if (c.p.softmax_scale <= 0.f) c.p.softmax_scale = 1.0f / __builtin_sqrtf((float)p->head_dim);
-    c.page_shift = __builtin_ctz((unsigned)rows);
-    c.aug_len = (int32_t)augmented(p);
-    c.cu_rows = cu_rows, c.start = start, c.total_rows = (int32_t)total_rows;
-    return KSA_OK;
-}
-
-// {row, head} strides in elements of a [rows, heads, head_dim] bf16 tensor
-int check_strides(int64_t out[2], const int64_t *given, int32_t heads, int32_t head_dim) {
-    out[0] = given ? given[0] : (int64_t)heads * head_dim, out[1] = given ? given[1] : head_dim;
-    return out[0] > 0 && out[1] > 0 && out[0] % 8 == 0 && out[1] % 8 == 0 ? KSA_OK : KSA_ERR_INVALID_ARG;
-}
 
 // Keys that so many consecutive rows of a sequence see together, none less: the summaries, the text of the window and of the rows.
 int64_t most_keys(const ksa_params *p, int64_t rows) {
@@ -152,8 +96,6 @@ KsaPagedPlan plan_paged(const ksa_params *p, int64_t total_rows, int64_t max_row
 
 bool bad_fwd(int64_t max_rows, int32_t n_splits) { return max_rows <= 0 || n_splits < 0 || n_splits > 1024; }
 
-constexpr int64_t MOST_LANES = (int64_t)1 << 32;   // of a grid, none of its dimensions more
-
 bool too_large(const ksa_params *p, int64_t total_rows, const KsaPagedPlan &plan) {
     if (plan.n_splits > 1 && total_rows * p->n_q_heads * (plan.n_splits > 8 ? 256 : 64) >= MOST_LANES) return true;
     return !plan.few && (int64_t)plan.slots * plan.n_splits * p->n_kv_heads * plan.pairs * 2 * plan.groups >= MOST_LANES;
@@ -162,16 +104,6 @@ bool too_large(const ksa_params *p, int64_t total_rows, const KsaPagedPlan &plan
 size_t span_bytes(const ksa_params *p, int64_t total_rows) { return (size_t)total_rows * p->n_q_heads * ksa_paged_record(p->head_dim) * sizeof(float); }
 size_t workspace_of(const ksa_params *p, int64_t total_rows, const KsaPagedPlan &plan) {
     return plan.n_splits == 1 ? 0 : plan.n_splits * span_bytes(p, total_rows);
-}
-
-int move_call(KsaPagedMove &a, const ksa_params *p, const ksa_paged_cache *cache, const void *k, const void *v, const int64_t *strides,
-              const int32_t *cu_rows, const int32_t *start, int64_t total_rows) {
-    const int rc = check_call(a.call, p, cache, cu_rows, start, total_rows);
-    if (rc != KSA_OK) return rc;
-    if (total_rows > 0 && (!k || !v)) return KSA_ERR_INVALID_ARG;
-    if (!aligned(k, 16) || !aligned(v, 16)) return KSA_ERR_INVALID_ARG;
-    if ((total_rows * p->head_dim / 2048 + 1) * p->n_kv_heads * 256 >= MOST_LANES) return KSA_ERR_UNSUPPORTED;
-    return check_strides(a.strides, strides, p->n_kv_heads, p->head_dim);
 }
 
 }  // namespace

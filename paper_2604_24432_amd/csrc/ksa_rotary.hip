@@ -1,0 +1,84 @@
+// Rotary positions of whole augmented sequences, there and back.  Data movement, bound by HBM: a wave has a row, or a part of its heads; its lanes work out
+// the row's cosines and sines, one pair each, share them in LDS and then go over the heads, 16 bytes of one per lane.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "ksa_rotary.h"
+
+namespace {
+
+struct Args {
+    RotaryArgs rotary;
+    const __bf16 *in[2];
+    __bf16 *out[2];
+    int64_t in_batch[2], in_row[2], in_head[2], out_batch[2], out_row[2], out_head[2];
+    int32_t heads[2];
+    int32_t rows, units, parts;   // rows of a sequence; rows of all times parts
+    int32_t c;
+    float sign;
+    KsaDivisor by_parts, by_rows, by_w;
+    int32_t w;
+};
+
+template <int D, int P>
+__global__ __launch_bounds__(256) void ksa_rotary_kernel(const Args a) {
+    constexpr int LANES = D / 8, PER = 64 / LANES, AT_ONCE = 4;   // lanes of a head, heads of a wave's access, accesses on their way
+    __shared__ __align__(16) float table[4][64][2];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int unit = (int)blockIdx.x * 4 + wave;
+    if (unit >= a.units) return;
+    const int row = ksa_div(unit, a.by_parts), part = unit - row * a.parts, b = ksa_div(row, a.by_rows), at = row - b * a.rows;
+    const int j = ksa_div(at, a.by_w), position = j * a.c + min(at - j * a.w, a.c - 1);
+    const int piece = lane % LANES;
+    const Turn t = turn_at<P>(a.rotary, position, a.sign, piece, table[wave]);
+    const int all = a.heads[0] + a.heads[1], step = PER * a.parts;
+    for (int h0 = part * PER + lane / LANES; h0 < all; h0 += step * AT_ONCE) {
+        Piece<P> x[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int h = min(h0 + i * step, all - 1), of = h >= a.heads[0] ? 1 : 0, head = h - (of ? a.heads[0] : 0);
+            const __bf16 *const from = of ? a.in[1] + b * a.in_batch[1] + at * a.in_row[1] + head * a.in_head[1] : a.in[0] + b * a.in_batch[0] + at * a.in_row[0] + head * a.in_head[0];
+            x[i] = load_piece<P>(a.rotary, from, piece);
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int h = h0 + i * step, of = h >= a.heads[0] ? 1 : 0, head = h - (of ? a.heads[0] : 0);
+            if (h >= all) break;
+            __bf16 *const to = of ? a.out[1] + b * a.out_batch[1] + at * a.out_row[1] + head * a.out_head[1] : a.out[0] + b * a.out_batch[0] + at * a.out_row[0] + head * a.out_head[0];
+            *reinterpret_cast<u32x4 *>(to + piece * 8) = turned<P>(a.rotary, x[i], piece, t);
+        }
+    }
+}
+
+template <int D>
+void launch(const Args &a, int pairs, hipStream_t st) {
+    const dim3 grid((unsigned)((a.units + 3) / 4));
+    if (pairs == KSA_HALF) hipLaunchKernelGGL((ksa_rotary_kernel<D, KSA_HALF>), grid, dim3(256), 0, st, a);
+    else if (pairs == KSA_NEXT) hipLaunchKernelGGL((ksa_rotary_kernel<D, KSA_NEXT>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((ksa_rotary_kernel<D, KSA_HALF_ANY>), grid, dim3(256), 0, st, a);
+}
+
+}  // namespace
+
+int ksa_launch_rotary(const KsaRotaryCall &L, void *stream) {
+    Args a;
+    a.rotary = {L.rotary.turns, L.rotary.dim, L.rotary.magnitude};
+    for (int x = 0; x < 2; ++x) {
+        a.in[x] = static_cast<const __bf16 *>(L.in[x]), a.out[x] = static_cast<__bf16 *>(L.out[x]);
+        a.in_batch[x] = L.in_strides[x][0], a.in_row[x] = L.in_strides[x][1], a.in_head[x] = L.in_strides[x][2];
+        a.out_batch[x] = L.out_strides[x][0], a.out_row[x] = L.out_strides[x][1], a.out_head[x] = L.out_strides[x][2];
+    }
+    a.heads[0] = L.in[0] ? L.p.n_q_heads : 0, a.heads[1] = L.in[1] ? L.p.n_kv_heads : 0;
+    a.rows = L.aug_len;
+    const int rows = L.aug_len * L.p.batch, accesses = ((a.heads[0] + a.heads[1]) * L.p.head_dim + 511) / 512;
+    a.parts = std::max(1, std::min(accesses, 4096 / rows));
+    a.units = rows * a.parts;
+    a.c = L.p.chunk_len, a.w = a.c + (L.p.chunk_len > L.p.n_text ? 0 : L.p.n_summary);   // (a chunk that is never whole has no summaries)
+    a.sign = L.back ? -1.f : 1.f;
+    a.by_parts = ksa_divisor(a.parts), a.by_rows = ksa_divisor(a.rows), a.by_w = ksa_divisor(a.w);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (L.p.head_dim == 128) launch<128>(a, rotary_pairs(L.rotary), st);
+    else launch<64>(a, rotary_pairs(L.rotary), st);
+    return hipGetLastError() == hipSuccess ? KSA_OK : KSA_ERR_HIP;
+}

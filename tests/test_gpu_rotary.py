@@ -1,0 +1,254 @@
+"""GPU tests of rotary positions: whole sequences, there and back, and a serving step's rows, against definitions in 64 bits (tests/rotary.py)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_24432_amd as K
+from tests.paged import Pages, batch_of, randn
+from tests.paged_fp4 import Pages4
+from tests.rotary import RULES, handle, name, positions, turn
+from tests.test_gpu_paged import bits, say
+
+pytestmark = pytest.mark.gpu
+
+
+def within(got, x, rule, at, back=False):
+    want, off = turn(x.double(), rule, at, back)
+    err = (got.double() - want).abs()
+    assert bool((err <= off).all()), float((err - off).max())
+
+
+# batch, heads, KV heads, d, text tokens, c, m
+SHAPES = [(1, 1, 1, 128, 1, 64, 8), (2, 4, 2, 128, 150, 64, 8), (1, 12, 4, 64, 333, 48, 6), (3, 5, 1, 128, 40, 1, 0), (1, 32, 8, 128, 1000, 8, 1), (1, 33, 3, 64, 20, 100, 4)]
+
+
+@pytest.mark.parametrize("rule", RULES, ids=name)
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_whole_sequences(shape, rule):
+    B, Hq, Hkv, d, n, c, m = shape
+    rule = {**rule, "dim": min(rule["dim"], d)}
+    say(f"rotary whole {shape} {rule}")
+    p = K.make_params(B, n, c, m, 1, Hq, Hkv, d)
+    L = K.binding.augmented_rows(p, n)
+    at = positions(range(L), c, m)
+    assert at.tolist() == K.Layout(p).index_maps()["position_ids"].tolist()
+    r = handle(rule)
+    q, k = randn(B, L, Hq, d, seed=1), randn(B, L, Hkv, d, seed=2)
+    for back, call in ((False, K.ksa_rotary_fwd), (True, K.ksa_rotary_bwd)):
+        q0, k0 = q.clone(), k.clone()
+        q_out, k_out = call(p, r, q0, k0)
+        assert torch.equal(bits(q0), bits(q)) and torch.equal(bits(k0), bits(k))
+        within(q_out, q, rule, at, back), within(k_out, k, rule, at, back)
+        only_q, none = call(p, r, q, None)
+        none_, only_k = call(p, r, None, k)
+        assert none is None and none_ is None and torch.equal(bits(only_q), bits(q_out)) and torch.equal(bits(only_k), bits(k_out))
+        call(p, r, q0, k0, q0, k0)                       # in place
+        assert torch.equal(bits(q0), bits(q_out)) and torch.equal(bits(k0), bits(k_out))
+
+
+def test_strides_of_a_fused_projection():
+    say("rotary strides")
+    p = K.make_params(2, 100, 16, 2, 1, 4, 2, 128)
+    L = K.binding.augmented_rows(p, 100)
+    rule = RULES[3]
+    fused = randn(2, L, 9, 128, seed=1)
+    before = fused.clone()
+    q, k = fused[:, :, :4], fused[:, :, 4:6]
+    out = torch.full((2, 9, L, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    K.ksa_rotary_fwd(p, handle(rule), q, k, out[:, :4].transpose(1, 2), out[:, 5:7].transpose(1, 2))
+    at = positions(range(L), 16, 2)
+    within(out[:, :4].transpose(1, 2), q, rule, at), within(out[:, 5:7].transpose(1, 2), k, rule, at)
+    assert bool((out[:, 4] == 7).all()) and bool((out[:, 7:] == 7).all()) and torch.equal(bits(fused), bits(before))
+    K.ksa_rotary_fwd(p, handle(rule), q, k, q, k)
+    within(fused[:, :, :4], before[:, :, :4], rule, at), within(fused[:, :, 4:6], before[:, :, 4:6], rule, at)
+    assert torch.equal(bits(fused[:, :, 6:]), bits(before[:, :, 6:]))
+
+
+@pytest.mark.parametrize("rule", [RULES[0], RULES[3], RULES[4]], ids=name)
+def test_gradients_against_differences(rule):
+    """Linear in its input: <g, R (x + h e) - R x> / h is the gradient, to the roundings of both (float64 sums of the kernels' outputs)."""
+    say("rotary differences")
+    p = K.make_params(1, 50, 16, 2, 1, 2, 1, 128)
+    L = K.binding.augmented_rows(p, 50)
+    r = handle(rule)
+    g = randn(1, L, 2, 128, seed=3)
+    dq, _ = K.ksa_rotary_bwd(p, r, g, None)
+    zero, _ = K.ksa_rotary_fwd(p, r, torch.zeros_like(g), None)
+    assert bool((zero == 0).all())
+    picks = [(0, 0, 0), (17, 1, 5), (31, 0, 64), (L - 1, 1, 127), (40, 0, 9), (12, 1, 70)]
+    for row, head, e in picks:
+        x = torch.zeros_like(g)
+        x[0, row, head, e] = 1.0
+        y, _ = K.ksa_rotary_fwd(p, r, x, None)
+        diff = float((g.double() * y.double()).sum())
+        # the difference has two outputs, each off by half a step of bf16, the gradient has one such step
+        size = float((g.double() * y.double()).abs().sum())
+        assert abs(float(dq[0, row, head, e]) - diff) <= 2 ** -8 * (size + abs(diff)) + 2.0 ** -19 * float(g[0, row, head].abs().max()), (row, head, e)
+
+
+def test_no_numbers_stay_in_their_pairs():
+    say("rotary no numbers")
+    p = K.make_params(1, 30, 16, 2, 1, 2, 1, 64)
+    L = K.binding.augmented_rows(p, 30)
+    q = randn(1, L, 2, 64, seed=1)
+    for rule in (dict(dim=32), dict(dim=32, interleaved=True), dict(dim=20), dict(dim=22, interleaved=True)):
+        r = handle(rule)
+        y0, _ = K.ksa_rotary_fwd(p, r, q, None)
+        for e in (0, 5, rule["dim"] - 1, rule["dim"], 63):
+            x = q.clone()
+            x[0, 7, 1, e] = math.nan
+            y, _ = K.ksa_rotary_fwd(p, r, x, None)
+            hit = torch.zeros_like(y, dtype=torch.bool)
+            half = rule["dim"] // 2
+            pair = [e] if e >= rule["dim"] else [e, e ^ 1] if rule.get("interleaved") else [e, (e + half) % rule["dim"]]
+            hit[0, 7, 1, pair] = True
+            assert bool(torch.isnan(y[hit]).all()) and torch.equal(bits(y)[~hit], bits(y0)[~hit]), (rule, e)
+
+
+def test_far_positions():
+    """Rows of whole sequences near the end of a million positions, through the paged form too."""
+    say("rotary far")
+    n, c, m = 1 << 20, 64, 8
+    p = K.make_params(1, n, c, m, 1, 1, 1, 64)
+    L = K.binding.augmented_rows(p, n)
+    rows = np.concatenate([np.arange(5), np.arange(L // 3, L // 3 + 100), np.arange(L - 300, L)])
+    for rule in (dict(dim=64), dict(dim=64, base=1e6, interleaved=True), dict(dim=20, scaling="linear", factor=3.0)):
+        q = randn(1, L, 1, 64, seed=1)
+        out, _ = K.ksa_rotary_fwd(p, handle(rule), q, None)
+        within(out[:, rows], q[:, rows], rule, positions(rows, c, m))
+
+
+def make(p, n_rows, page, kind, seed):
+    return Pages4(p, n_rows, page, seed) if kind == "fp4" else Pages(p, n_rows, page, kind == "fp8", seed, fill=0.0)
+
+
+PLACES = [(1, 8, 1, 64, 8, 1, 16, [786], [1]), (6, 32, 8, 128, 64, 8, 64, [0, 1, 63, 64, 71, 72], [1] * 6), (4, 12, 4, 64, 48, 6, 8, [1500, 53, 160, 7], [77, 0, 301, 1]),
+          (2, 5, 5, 128, 1, 0, 16, [40, 3], [33, 90])]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "fp4"])
+@pytest.mark.parametrize("rule", [RULES[0], RULES[1], RULES[3], RULES[4], RULES[6]], ids=name)
+@pytest.mark.parametrize("case", PLACES, ids=lambda x: "x".join(map(str, x[:7])))
+def test_new_rows_into_pages(case, rule, kind):
+    """The same bits as turning (ksa_rotary_fwd's, by position) and ksa_paged_append; q to its bound."""
+    B, Hq, Hkv, d, c, m, page, first, count = case
+    rule = {**rule, "dim": min(rule["dim"], d)}
+    say(f"rotary place {case} {rule} {kind}")
+    p = K.make_params(B, 4096, c, m, 1, Hq, Hkv, d)
+    r = handle(rule)
+    total = sum(count)
+    q, k, v = randn(total + 2, Hq, d, seed=1), randn(total + 2, Hkv, d, seed=2), randn(total + 2, Hkv, d, seed=3)
+    cu, start = batch_of(first, count)
+    n_rows = [a + n for a, n in zip(first, count)]
+    got, want = make(p, n_rows, page, kind, 5), make(p, n_rows, page, kind, 5)
+    q_out = torch.full_like(q, 7.0)
+    K.ksa_paged_rotary(got.cache, r, q, k, v, cu, start, q_out=q_out)
+    assert bool((q_out[total:] == 7).all())
+    # k turned by the call for whole sequences, every row at its place
+    whole = K.make_params(1, 4096, c, m, 1, Hkv, Hkv, d)
+    L = K.binding.augmented_rows(whole, 4096)
+    at, k_turned = 0, k.clone()
+    for b, n in enumerate(count):
+        rows = list(range(first[b], first[b] + n))
+        within(q_out[at:at + n], q[at:at + n], rule, positions(rows, c, m))
+        line = torch.zeros(1, L, Hkv, d, dtype=torch.bfloat16, device="cuda")
+        line[0, rows] = k[at:at + n]
+        k_turned[at:at + n] = K.ksa_rotary_fwd(whole, r, None, line)[1][0, rows]
+        at += n
+    K.ksa_paged_append(want.cache, k_turned, v, cu, start)
+    for x in ("k", "v", "k_exp", "v_exp"):
+        a, b = getattr(got, x), getattr(want, x)
+        assert a is None or torch.equal(a.view(torch.uint8), b.view(torch.uint8)), x
+    # in place, without q, and strided
+    again = make(p, n_rows, page, kind, 5)
+    assert K.ksa_paged_rotary(again.cache, r, None, k, v, cu, start) is None
+    assert torch.equal(again.k.view(torch.uint8), got.k.view(torch.uint8))
+    fused = torch.cat([q, k, v], 1)
+    strided = make(p, n_rows, page, kind, 5)
+    K.ksa_paged_rotary(strided.cache, r, fused[:, :Hq], fused[:, Hq:Hq + Hkv], fused[:, Hq + Hkv:], cu, start, q_out=fused[:, :Hq])
+    assert torch.equal(bits(fused[:total, :Hq]), bits(q_out[:total])) and torch.equal(bits(fused[total:, :Hq]), bits(q[total:]))
+    assert torch.equal(strided.k.view(torch.uint8), got.k.view(torch.uint8)) and torch.equal(strided.v.view(torch.uint8), got.v.view(torch.uint8))
+
+
+def test_sequences_out_of_place_and_rows_without_a_page():
+    say("rotary out of place")
+    p = K.make_params(3, 500, 16, 2, 1, 4, 2, 64)
+    r = handle(dict(dim=64))
+    q, k, v = randn(30, 4, 64, seed=1), randn(30, 2, 64, seed=2), randn(30, 2, 64, seed=3)
+    pages = Pages(p, [200, 200, 200], 16, False, 5, fill=0.0)
+    cu, start = batch_of([100, -1, 10 ** 6], [10, 10, 10])
+    q_out = K.ksa_paged_rotary(pages.cache, r, q, k, v, cu, start)
+    within(q_out[:10], q[:10], dict(dim=64), positions(range(100, 110), 16, 2))
+    assert bool(torch.isnan(q_out[10:]).all())
+    assert int((pages.k != 0).any(-1).any(1).sum()) == 10
+    none = torch.full_like(pages.text_dev, -1)
+    empty = K.PagedCache(p, torch.zeros_like(pages.k), torch.zeros_like(pages.v), none, torch.full_like(pages.sums_dev, -1))
+    q_out = K.ksa_paged_rotary(empty, r, q, k, v, *batch_of([100, 50, 0], [10, 10, 10]))
+    assert bool(torch.isfinite(q_out).all()) and not bool(empty.k.any())
+    assert K.ksa_paged_rotary(empty, r, q[:0], k[:0], v[:0], *batch_of([0, 0, 0], [0, 0, 0])).shape[0] == 0
+
+
+def test_graph_and_streams():
+    """Captured with a training step's eager calls beside it; replays with new data give the eager bits."""
+    say("rotary graph")
+    p = K.make_params(1, 200, 16, 2, 1, 4, 2, 128)
+    L = K.binding.augmented_rows(p, 200)
+    r = handle(RULES[0])
+    q, k = randn(1, L, 4, 128, seed=1), randn(1, L, 2, 128, seed=2)
+    q_out, k_out, dq, dk = torch.empty_like(q), torch.empty_like(k), torch.empty_like(q), torch.empty_like(k)
+    pages = Pages(p, [L], 16, False, 5, fill=0.0)
+    cu, start = batch_of([0], [9])
+
+    def step():
+        K.ksa_rotary_fwd(p, r, q, k, q_out, k_out)
+        K.ksa_rotary_bwd(p, r, q_out, k_out, dq, dk)
+        K.ksa_paged_rotary(pages.cache, r, q[0, :9], k[0, :9], k[0, :9], cu, start, q_out=q_out[0, :9])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for x in range(4):
+        q.copy_(randn(1, L, 4, 128, seed=10 + x)), k.copy_(randn(1, L, 2, 128, seed=20 + x))
+        start.fill_(7 * x)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (q_out, k_out, dq, dk, pages.k)]
+        pages.k.zero_()
+        step()
+        pages_k = pages.k.clone()
+        for a, b in zip(got[:4], (q_out, k_out, dq, dk)):
+            assert torch.equal(bits(a), bits(b))
+        written = (pages_k != 0).any(-1)
+        assert torch.equal(bits(got[4][written]), bits(pages_k[written]))
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    a, b = K.ksa_rotary_fwd(p, r, q, k, stream=stream)
+    c = K.ksa_paged_rotary(pages.cache, r, q[0, :9], k[0, :9], k[0, :9], cu, start, stream=stream)
+    stream.synchronize()
+    want = K.ksa_rotary_fwd(p, r, q, k)
+    assert torch.equal(bits(a), bits(want[0])) and torch.equal(bits(b), bits(want[1])) and bool(torch.isfinite(c).all())
+
+
+def test_python_refuses_what_does_not_fit():
+    p = K.make_params(1, 100, 16, 2, 1, 4, 2, 128)
+    L = K.binding.augmented_rows(p, 100)
+    r = handle(RULES[0])
+    q, k = randn(1, L, 4, 128), randn(1, L, 2, 128)
+    for bad in ((q[:, 1:], k), (q, q), (q.float(), k), (None, None), (q, k[..., :64]), (q.cpu(), k), (q, k, q[:, :1]), (q, None, None, k)):
+        with pytest.raises(ValueError):
+            K.ksa_rotary_fwd(p, r, *bad)
+    with pytest.raises(K.KsaError):
+        K.ksa_rotary_fwd(K.make_params(1, 100, 16, 2, 1, 4, 2, 64), r, q[..., :64].contiguous(), None)      # dim beyond the head
+    pages = Pages(p, [100], 16, False, 5)
+    cu, start = batch_of([0], [5])
+    x, y = q[0, :5], k[0, :5]
+    for bad in ((x, y, y[:4], cu, start), (x[:4], y, y, cu, start), (x, y, y, cu[:1], start), (x, y, y, cu.long(), start), (None, y, y, cu, start, x), (y, y, y, cu, start)):
+        with pytest.raises(ValueError):
+            K.ksa_paged_rotary(pages.cache, r, *bad)
