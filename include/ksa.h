@@ -353,7 +353,8 @@ typedef struct ksa_paged_cache {
     void *k, *v;                    /* device, bf16, e4m3 or pairs of e2m1, [n_pages, Hkv, page_rows, d (pairs: d / 2)], last dim contiguous */
     uint8_t *k_exp, *v_exp;         /* device, contiguous: [n_pages, Hkv, page_rows] for KSA_CACHE_FP8, [n_pages, Hkv, page_rows, d / 32] (on 4 bytes)
                                        for KSA_CACHE_FP4, else NULL */
-    int64_t strides[3];             /* of k and v: {page, head, row} in elements (KSA_CACHE_FP4: bytes), multiples of 16 bytes; {0, 0, 0} = contiguous */
+    int64_t strides[3];             /* of k and v: {page, head, row} in elements, multiples of 16 bytes; {0, 0, 0} = contiguous.  KSA_CACHE_FP4: in bytes;
+                                       UNSUPPORTED if the page's, or page_rows times the row's, exceeds 2^32 - 1 */
 } ksa_paged_cache;
 
 /*

@@ -49,6 +49,7 @@ inline int check_cache(KsaPagedCall &c, const ksa_params *p, const ksa_paged_cac
             c.cache_strides[x] = s[x] * size;
         }
     }
+    if (f4 && (c.cache_strides[0] > UINT32_MAX || c.cache_strides[2] > UINT32_MAX / rows)) return KSA_ERR_UNSUPPORTED;   // (places in a page are 32 bits)
     c.p = *p, c.cache = *cache;
     if (c.p.softmax_scale <= 0.f) c.p.softmax_scale = 1.0f / __builtin_sqrtf((float)p->head_dim);
     c.page_shift = __builtin_ctz((unsigned)rows);

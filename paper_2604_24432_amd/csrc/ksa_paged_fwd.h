@@ -35,7 +35,6 @@ struct FwdArgs {
     int64_t q_row, q_head, o_row, o_head;
     int32_t max_rows;
     int32_t n_q_heads, n_kv_heads, group, n_splits;
-    int32_t groups;               // 4-bit rows: exponents of a row
     KsaDivisor by_group, by_heads, by_splits, by_q_heads;
     float q_scale, score_scale;   // scale * log2(e) in two factors, the first a power of two that goes into q
 };
@@ -52,7 +51,7 @@ constexpr int MOST_EXP4 = 127 + 125, NO_NUMBERS = 255;
 constexpr bool is_fp8(int format) { return format == KSA_CACHE_FP8; }
 constexpr bool is_fp4(int format) { return format == KSA_CACHE_FP4; }
 constexpr int bytes_of(int format, int elements) { return is_fp4(format) ? elements / 2 : is_fp8(format) ? elements : elements * 2; }
-constexpr int PARTS[] = {1, 2, 4};   // pieces of 8 bf16 that 16 bytes of a row become, by format
+constexpr int PARTS[] = {1, 2};   // pieces of 8 bf16 that 16 bytes of a row become, by format
 
 __device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
     const unsigned lo = (unsigned)__shfl((int)(unsigned)x, lane), hi = (unsigned)__shfl((int)(unsigned)(x >> 32), lane);
@@ -64,13 +63,10 @@ __device__ __forceinline__ int64_t spot_exp(const FwdArgs &a, const Spot &s, int
     return (((int64_t)max(s.page, 0) * a.n_kv_heads + hkv) << a.rows.shift) + s.slot;
 }
 
-// Sixteen bytes of a cache row as bf16: 8 elements, 16 of an 8-bit row, 32 of a 4-bit one.
+// Sixteen bytes of a cache row as bf16: 8 elements, or 16 of an 8-bit row.
 template <int F>
 __device__ __forceinline__ void as_bf16(const u32x4 &x, float scale, u32x4 (&y)[PARTS[F]]) {
-    if constexpr (is_fp4(F)) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = unpack_fp4(x[e], scale);
-    } else if constexpr (is_fp8(F)) {
+    if constexpr (is_fp8(F)) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const u32x2 z = unpack_fp8(x[e], scale);
@@ -111,20 +107,21 @@ __device__ __forceinline__ bool take_out_raw(u32x4 &x) {
     return any != 0;
 }
 
-// A 4-bit group that is no numbers becomes zeros; exponents beyond the largest count as that one.
-__device__ __forceinline__ bool take_out_group(u32x4 &x, int &e) {
+// A part of a 4-bit group that is no numbers becomes zeros; exponents beyond the largest count as that one.
+template <int WORDS, class T>
+__device__ __forceinline__ bool take_out_group(T &x, int &e) {
     const bool odd = e == NO_NUMBERS;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = odd ? 0u : x[i];
+    for (int i = 0; i < WORDS; ++i) x[i] = odd ? 0u : x[i];
     e = min(e, MOST_EXP4);
     return odd;
 }
 
 // four elements of a V row from column d on; those that are numbers are zero
-template <int F>
+template <int D, int F>
 __device__ __forceinline__ void no_numbers(const FwdArgs &a, int hkv, const Spot &s, int d, float (&y)[4]) {
     if constexpr (is_fp4(F)) {
-        const bool odd = a.v_exp[spot_exp(a, s, hkv) * a.groups + d / 32] == NO_NUMBERS;
+        const bool odd = a.v_exp[spot_exp(a, s, hkv) * (D / 32) + d / 32] == NO_NUMBERS;
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = odd ? __builtin_nanf("") : 0.f;
         return;
@@ -203,7 +200,7 @@ __device__ __forceinline__ void add_no_numbers(const FwdArgs &a, int hkv, const 
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             float z[4];
-            no_numbers<F>(a, hkv, at, db * 32 + 8 * g + 4 * h, z);
+            no_numbers<D, F>(a, hkv, at, db * 32 + 8 * g + 4 * h, z);
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[db][4 * g + e] += see ? z[e] : 0.f;
         }
@@ -252,8 +249,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ksa_paged_few_kernel(const 
     const unsigned char *const kb = a.k + hkv * a.head_bytes, *const vb = a.v + hkv * a.head_bytes;
     const int f_row = lane / LPR, f_piece = lane % LPR;
     u32x4 kr[NI], vr[NI];
-    int ke = 0, ve = 0;        // 8-bit rows: exponents of row lane % 32
-    int kes[NI], ves[NI];      // 4-bit rows: of the lane's pieces
+    int ke = 0, ve = 0;        // exponents of row lane % 32
     unsigned lost = 0;         // keys without a page
     // Loads return in the order they are issued in: a block's table entries are asked for before the rows of the block in front of it.
     Entry entry;               // of row lane % 32 of the block to be requested next
@@ -266,14 +262,6 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ksa_paged_few_kernel(const 
         if constexpr (is_fp8(F)) {
             const int64_t at = spot_exp(a, spot, hkv);
             ke = a.k_exp[at], ve = a.v_exp[at];
-        }
-        if constexpr (is_fp4(F)) {
-            const int64_t at = spot_exp(a, spot, hkv) * LPR;
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int64_t mine = lane_value(at, i * RPI + f_row) + f_piece;
-                kes[i] = a.k_exp[mine], ves[i] = a.v_exp[mine];
-            }
         }
         int64_t from[NI];
 #pragma unroll
@@ -310,7 +298,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ksa_paged_few_kernel(const 
     unsigned char *const put_k_at = own + f_row * KROW + f_piece * 16 * PARTS[F], *const put_v_at = own + BLOCK * KROW + f_row * VROW + f_piece * 16 * PARTS[F];
     auto put = [&](const u32x4 &x, int e, int i, unsigned char *to) {
         u32x4 y[PARTS[F]];
-        as_bf16<F>(x, is_fp4(F) ? power_of_two(e) : is_fp8(F) ? power_of_two(__shfl(e, i * RPI + f_row)) : 1.f, y);
+        as_bf16<F>(x, is_fp8(F) ? power_of_two(__shfl(e, i * RPI + f_row)) : 1.f, y);
 #pragma unroll
         for (int z = 0; z < PARTS[F]; ++z) *reinterpret_cast<u32x4 *>(to + z * 16) = y[z];
     };
@@ -323,13 +311,13 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void ksa_paged_few_kernel(const 
             if (is_fp8(F)) ve = min(ve, MOST_EXP);
             bool odd = false;
 #pragma unroll
-            for (int i = 0; i < NI; ++i) odd |= is_fp4(F) ? take_out_group(vr[i], ves[i]) : take_out_raw<F>(vr[i]);
+            for (int i = 0; i < NI; ++i) odd |= take_out_raw<F>(vr[i]);
             ever |= __builtin_amdgcn_ballot_w64(odd) != 0;
         }
 #pragma unroll
-        for (int i = 0; i < NI; ++i) put(kr[i], is_fp4(F) ? kes[i] : ke, i, put_k_at + i * RPI * KROW);
+        for (int i = 0; i < NI; ++i) put(kr[i], ke, i, put_k_at + i * RPI * KROW);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) put(vr[i], is_fp4(F) ? ves[i] : ve, i, put_v_at + i * RPI * VROW);
+        for (int i = 0; i < NI; ++i) put(vr[i], ve, i, put_v_at + i * RPI * VROW);
         if (x + STEP < v1) request(x + 2 * STEP);
 
         f32x16 sc;
@@ -488,7 +476,10 @@ template <int D, int F, int NW, int GROUPS>
 __global__ __launch_bounds__(NW * GROUPS * 64, 2) void ksa_paged_many_kernel(const FwdArgs a) {
     constexpr int KS = D / 16, DB = D / 32, PAIRS = NW * 32;
     constexpr int RW = BN / NW;                                       // rows of a tile that a wave fetches
-    constexpr int LPR = bytes_of(F, D) / 16, RPI = 64 / LPR < RW ? 64 / LPR : RW, NI = RW / RPI;   // lanes per row, rows per load, loads per wave and tensor
+    constexpr int EACH = is_fp4(F) ? D / (2 * NW) : 16;               // bytes of a row per lane and load; a wave's rows of 4 bits are one load
+    constexpr int LPR = bytes_of(F, D) / EACH, RPI = 64 / LPR < RW ? 64 / LPR : RW, NI = RW / RPI;   // lanes per row, rows per load, loads per wave and tensor
+    constexpr int AS_BF16 = EACH * 2 * D / bytes_of(F, D);            // what they are as bf16
+    typedef unsigned piece_t __attribute__((ext_vector_type(EACH / 4)));
     constexpr int KROW = TileRow<D>::K, VROW = TileRow<D>::V, K_BYTES = BN * KROW, V_BYTES = BN * VROW;
     constexpr int STAGE_ROW = D * 2 + 16;
     static_assert(RW % RPI == 0 && NI >= 1, "a wave's rows are whole loads");
@@ -554,7 +545,7 @@ __global__ __launch_bounds__(NW * GROUPS * 64, 2) void ksa_paged_many_kernel(con
     static_assert(!is_fp4(F) || NI == 1, "4-bit rows: the exponents of the lane's one piece");
     int k_e = 0, v_e = 0, next_k_e = 0, next_v_e = 0;
     int64_t from[NI];                          // where the rows of the lane's loads lie: of the K tile asked for last, then of the V tile
-    u32x4 k_rows[NI], v_rows[NI];
+    piece_t k_rows[NI], v_rows[NI];
     bool lost = false, next_lost = false, odd = false;   // row lane % RW of the K tile on its way has no page; elements of V were taken out
     const int last = min(keys.n, end_tile * BN) - 1;
     auto look = [&](int t) { entry = entry_of(a.rows, tile.b, key_at(keys, min(t * BN + RW * wave + lane % RW, last))); };
@@ -563,9 +554,9 @@ __global__ __launch_bounds__(NW * GROUPS * 64, 2) void ksa_paged_many_kernel(con
         next_lost = spot.page < 0;
         next_at = spot_bytes(a, spot);
         if constexpr (is_fp8(F)) exp_at = spot_exp(a, spot, hkv);
-        if constexpr (is_fp4(F)) exp_at = lane_value(spot_exp(a, spot, hkv) * LPR, f_row) + f_piece;
+        if constexpr (is_fp4(F)) exp_at = lane_value(spot_exp(a, spot, hkv) * (D / 32), f_row) + f_piece * EACH / 16;
     };
-    auto find = [&](int i) { from[i] = lane_value(next_at, i * RPI + f_row) + f_piece * 16; };
+    auto find = [&](int i) { from[i] = lane_value(next_at, i * RPI + f_row) + f_piece * EACH; };
     auto load_exps = [&]() {
         if constexpr (F != KSA_CACHE_BF16) next_k_e = a.k_exp[exp_at], next_v_e = a.v_exp[exp_at];
     };
@@ -573,15 +564,20 @@ __global__ __launch_bounds__(NW * GROUPS * 64, 2) void ksa_paged_many_kernel(con
         if constexpr (is_fp8(F)) k_e = next_k_e, v_e = min(next_v_e, MOST_EXP);
         if constexpr (is_fp4(F)) k_e = next_k_e, v_e = next_v_e;
     };
-    auto load_k = [&](int i) { k_rows[i] = *reinterpret_cast<const u32x4 *>(kb + from[i]); };
-    auto load_v = [&](int i) { v_rows[i] = *reinterpret_cast<const u32x4 *>(vb + from[i]); };
-    auto put = [&](const u32x4 &x, int e, int i, unsigned char *to) {
-        u32x4 y[PARTS[F]];
-        as_bf16<F>(x, is_fp4(F) ? power_of_two(e) : is_fp8(F) ? power_of_two(__shfl(e, i * RPI + f_row)) : 1.f, y);
+    auto load_k = [&](int i) { k_rows[i] = *reinterpret_cast<const piece_t *>(kb + from[i]); };
+    auto load_v = [&](int i) { v_rows[i] = *reinterpret_cast<const piece_t *>(vb + from[i]); };
+    auto put = [&](const piece_t &x, int e, int i, unsigned char *to) {
+        if constexpr (is_fp4(F)) {
 #pragma unroll
-        for (int z = 0; z < PARTS[F]; ++z) *reinterpret_cast<u32x4 *>(to + z * 16) = y[z];
+            for (int z = 0; z < EACH / 4; ++z) *reinterpret_cast<u32x4 *>(to + z * 16) = unpack_fp4(x[z], power_of_two(e));
+        } else {
+            u32x4 y[PARTS[F]];
+            as_bf16<F>(x, is_fp8(F) ? power_of_two(__shfl(e, i * RPI + f_row)) : 1.f, y);
+#pragma unroll
+            for (int z = 0; z < PARTS[F]; ++z) *reinterpret_cast<u32x4 *>(to + z * 16) = y[z];
+        }
     };
-    const int put_k_at = (RW * wave + f_row) * KROW + f_piece * 16 * PARTS[F], put_v_at = 2 * K_BYTES + (RW * wave + f_row) * VROW + f_piece * 16 * PARTS[F];
+    const int put_k_at = (RW * wave + f_row) * KROW + f_piece * AS_BF16, put_v_at = 2 * K_BYTES + (RW * wave + f_row) * VROW + f_piece * AS_BF16;
     auto put_k = [&](int t, int i) { put(k_rows[i], k_e, i, lds + (t & 1) * K_BYTES + put_k_at + i * RPI * KROW); };
     auto put_v = [&](int t, int i) { put(v_rows[i], v_e, i, lds + (t & 1) * V_BYTES + put_v_at + i * RPI * VROW); };
     auto put_state = [&](int t) {   // with K tile t and V tile t - 1
@@ -722,7 +718,10 @@ __global__ __launch_bounds__(NW * GROUPS * 64, 2) void ksa_paged_many_kernel(con
                 odd = false;
                 if (!tile_all.sees_all(t * BN, t * BN + BN)) {
 #pragma unroll
-                    for (int i = 0; i < NI; ++i) odd |= is_fp4(F) ? take_out_group(v_rows[i], v_e) : take_out_raw<F>(v_rows[i]);
+                    for (int i = 0; i < NI; ++i) {
+                        if constexpr (is_fp4(F)) odd |= take_out_group<EACH / 4>(v_rows[i], v_e);
+                        else odd |= take_out_raw<F>(v_rows[i]);
+                    }
                 }
             }
             if (x >= 2 * KS - NI) put_v(t, x - (2 * KS - NI)), load_v(x - (2 * KS - NI));
@@ -870,7 +869,6 @@ FwdArgs fwd_args(const KsaPagedFwd &L) {
     int exponent = 0;
     (void)std::frexp(scale, &exponent);
     a.q_scale = std::ldexp(1.f, std::max(std::min(exponent - 1, 0), -8)), a.score_scale = scale / a.q_scale;
-    a.groups = p.head_dim / 32;
     return a;
 }
 
