@@ -655,25 +655,33 @@ def _check_stream(cache: PagedCache, stream):
         raise ValueError("stream belongs to another device than the cache")
 
 
-def _paged(cache: PagedCache, name, stream, *args):
-    """The call, on the cache's device: on `stream`, or on that device's current one."""
+def _on_device(dev, name, stream, *args):
+    """The call on device `dev`: on `stream`, or on that device's current one."""
     from torch import _C
-    here, there = _C._cuda_getDevice(), cache._dev
+    here = _C._cuda_getDevice()
     if stream is None:
-        raw = _C._cuda_getCurrentRawStream(there)
+        raw = _C._cuda_getCurrentRawStream(dev)
+    elif stream.device.index != dev:
+        raise ValueError("stream belongs to another device than the tensors")
     else:
-        _check_stream(cache, stream)
         raw = stream.cuda_stream
-    if here == there:
-        rc = getattr(lib(), name)(*cache._args, *args, raw)
+    if here == dev:
+        rc = getattr(lib(), name)(*args, raw)
     else:
-        _C._cuda_setDevice(there)
+        _C._cuda_setDevice(dev)
         try:
-            rc = getattr(lib(), name)(*cache._args, *args, raw)
+            rc = getattr(lib(), name)(*args, raw)
         finally:
             _C._cuda_setDevice(here)
     if rc:
         _check(rc, name)
+
+
+def _paged(cache: PagedCache, name, stream, *args):
+    """The call, on the cache's device."""
+    if stream is not None:
+        _check_stream(cache, stream)
+    _on_device(cache._dev, name, stream, *cache._args, *args)
 
 
 def ksa_paged_append(cache: PagedCache, k_new, v_new, cu_rows, start, stream=None):
@@ -788,28 +796,6 @@ class Rotary:
         return self.struct.dim
 
 
-def _on_device(dev, name, stream, *args):
-    """The call on device `dev`: on `stream`, or on that device's current one."""
-    from torch import _C
-    here = _C._cuda_getDevice()
-    if stream is None:
-        raw = _C._cuda_getCurrentRawStream(dev)
-    elif stream.device.index != dev:
-        raise ValueError("stream belongs to another device than the tensors")
-    else:
-        raw = stream.cuda_stream
-    if here == dev:
-        rc = getattr(lib(), name)(*args, raw)
-    else:
-        _C._cuda_setDevice(dev)
-        try:
-            rc = getattr(lib(), name)(*args, raw)
-        finally:
-            _C._cuda_setDevice(here)
-    if rc:
-        _check(rc, name)
-
-
 def _rotary_call(name, params: ksa_params, rotary: Rotary, tensors, outputs, names, stream):
     import torch
     if tensors[0] is None and tensors[1] is None:
@@ -819,25 +805,37 @@ def _rotary_call(name, params: ksa_params, rotary: Rotary, tensors, outputs, nam
             raise ValueError("stream belongs to another device than the tensors")
         with torch.cuda.stream(stream):      # what is allocated here belongs to `stream`
             return _rotary_call(name, params, rotary, tensors, outputs, names, None)
-    rows = augmented_rows(params, params.n_text)
-    out, ptr, strides = [], [], []
-    for x, y, what, heads in zip(tensors, outputs, names, (params.n_q_heads, params.n_kv_heads)):
+    (q, k), (q_out, k_out) = tensors, outputs
+    batch, n_text, c, m, _, _, n_q_heads, n_kv_heads, d = _FIELDS.unpack_from(params)
+    rows = n_text // c * (c + m) + n_text % c if c > 0 else -1
+    if q is not None and q_out is None:
+        q_out = torch.empty_like(q)
+    if k is not None and k_out is None:
+        k_out = torch.empty_like(k)
+    dev, shapes, plain = rotary._dev, ((batch, rows, n_q_heads, d), (batch, rows, n_kv_heads, d)), True
+    for x, y, shape in ((q, q_out, shapes[0]), (k, k_out, shapes[1])):     # as in _plain: in as few steps as possible
         if x is None:
-            if y is not None:
-                raise ValueError(f"an output is given for {what}, which is missing")
-            out.append(None), ptr.append((None, None)), strides.append((None, None))
-            continue
-        y = torch.empty_like(x) if y is None else y
-        for t in (x, y):
-            _require(t, what, torch.bfloat16, 4)
-            if tuple(t.shape) != (params.batch, rows, heads, params.head_dim):
-                raise ValueError(f"{what}: expected {(params.batch, rows, heads, params.head_dim)}, got {tuple(t.shape)}")
-            if t.get_device() != rotary._dev:
-                raise ValueError(f"{what} lies on another device than the frequencies")
-        out.append(y), ptr.append((x.data_ptr(), y.data_ptr())), strides.append((_strides_of(x), _strides_of(y)))
-    (q, q_out), (k, k_out) = ptr
-    _on_device(rotary._dev, name, stream, C.byref(params), rotary._arg, q, k, q_out, k_out, strides[0][0], strides[1][0], strides[0][1], strides[1][1])
-    return tuple(out)
+            plain = plain and y is None
+        else:
+            plain = plain and (x.dtype is torch.bfloat16 and y.dtype is torch.bfloat16 and x.shape == shape and y.shape == shape and x.is_contiguous() and
+                               y.is_contiguous() and x.get_device() == dev and y.get_device() == dev)
+    strides = (None,) * 4
+    if not plain:
+        augmented_rows(params, n_text)   # (parameters that make no sense are reported under this name)
+        for x, y, what, shape in ((q, q_out, names[0], shapes[0]), (k, k_out, names[1], shapes[1])):
+            if x is None:
+                if y is not None:
+                    raise ValueError(f"an output is given for {what}, which is missing")
+                continue
+            for t in (x, y):
+                _require(t, what, torch.bfloat16, 4)
+                if tuple(t.shape) != shape:
+                    raise ValueError(f"{what}: expected {shape}, got {tuple(t.shape)}")
+                if t.get_device() != dev:
+                    raise ValueError(f"{what} lies on another device than the frequencies")
+        strides = tuple(_strides_of(t) if t is not None else None for t in (q, k, q_out, k_out))
+    _on_device(dev, name, stream, C.byref(params), rotary._arg, *(t.data_ptr() if t is not None else None for t in (q, k, q_out, k_out)), *strides)
+    return q_out, k_out
 
 
 def ksa_rotary_fwd(params: ksa_params, rotary: Rotary, q, k, q_out=None, k_out=None, stream=None):
@@ -871,9 +869,12 @@ def ksa_paged_rotary(cache: PagedCache, rotary: Rotary, q, k_new, v_new, cu_rows
         if q_out is not None:
             raise ValueError("q_out is given, q is missing")
     else:
+        plain = q.dtype is torch.bfloat16 and q.shape[1:] == cache._q and q.is_contiguous() and q.get_device() == cache._dev
         if q_out is None:
             q_out = torch.empty_like(q)
-        if not cache._plain(q, q_out, cache._q, cu_rows, start):
+        else:
+            plain = plain and q_out.dtype is torch.bfloat16 and q_out.shape == q.shape and q_out.is_contiguous() and q_out.get_device() == cache._dev
+        if not plain:
             _rows_of_call(cache, ((q, "q"), (q_out, "q_out")), cache.params.n_q_heads, cu_rows, start)
             q_strides, out_strides = _strides_of(q), _strides_of(q_out)
         if q.shape[0] != k_new.shape[0]:
@@ -903,8 +904,8 @@ def paged_advance_workspace_bytes(cache: PagedCache) -> int:
 def _new_step(cache: PagedCache, total_rows: int) -> PagedStep:
     import torch
     batch = cache._batch[1][0]
-    i32 = lambda n: torch.empty(n, dtype=torch.int32, device=cache.device)  # noqa: E731
-    return PagedStep(i32(batch + 1), i32(batch), i32(1), torch.empty(total_rows, dtype=torch.int64, device=cache.device), i32(total_rows), i32(total_rows))
+    parts = torch.empty(2 * batch + 2 + 2 * total_rows, dtype=torch.int32, device=cache.device).split((batch + 1, batch, 1, total_rows, total_rows))
+    return PagedStep(*parts[:3], torch.empty(total_rows, dtype=torch.int64, device=cache.device), *parts[3:])
 
 
 def ksa_paged_advance(cache: PagedCache, page_refs, held, new_text, total_rows: int, step: Optional[PagedStep] = None, workspace=None, stream=None) -> PagedStep:
@@ -919,19 +920,18 @@ def ksa_paged_advance(cache: PagedCache, page_refs, held, new_text, total_rows: 
             return ksa_paged_advance(cache, page_refs, held, new_text, total_rows, step, workspace)
     if total_rows < 0:
         raise ValueError("total_rows must not be negative")
-    batch = cache._batch[1]
+    i32, dev, (cu_shape, batch), n_pages = torch.int32, cache._dev, cache._batch, cache.struct.n_pages
+    if not (page_refs.dtype is i32 and held.dtype is i32 and new_text.dtype is i32 and page_refs.shape == (n_pages,) and held.shape == batch and
+            new_text.shape == batch and page_refs.is_contiguous() and held.is_contiguous() and new_text.is_contiguous() and
+            page_refs.get_device() == dev and held.get_device() == dev and new_text.get_device() == dev):
+        raise ValueError(f"page_refs, held and new_text must be contiguous int32 of {n_pages}, {batch[0]} and {batch[0]} elements on the cache's device")
     if step is None:
         step = _new_step(cache, total_rows)
-        tensors = ((page_refs, "page_refs", (cache.struct.n_pages,)), (held, "held", batch), (new_text, "new_text", batch))
     else:
         rows = (total_rows,)
-        tensors = ((page_refs, "page_refs", (cache.struct.n_pages,)), (held, "held", batch), (new_text, "new_text", batch), (step.cu_rows, "cu_rows", cache._batch[0]),
-                   (step.start, "start", batch), (step.lacking, "lacking", (1,)), (step.positions, "positions", rows), (step.tokens, "tokens", rows))
-        if step.slots.dtype is not torch.int64 or step.slots.shape != rows or not step.slots.is_contiguous() or step.slots.get_device() != cache._dev:
-            raise ValueError(f"slots must be contiguous int64 {rows} on the cache's device")
-    for t, name, shape in tensors:
-        if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous() or t.get_device() != cache._dev:
-            raise ValueError(f"{name} must be contiguous int32 {tuple(shape)} on the cache's device")
+        for t, name, dtype, shape in zip(step, PagedStep._fields, (i32, i32, i32, torch.int64, i32, i32), (cu_shape, batch, (1,), rows, rows, rows)):
+            if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
+                raise ValueError(f"{name} must be contiguous {dtype} {shape} on the cache's device")
     if workspace is None:
         workspace = torch.empty(paged_advance_workspace_bytes(cache), dtype=torch.uint8, device=cache.device)
     elif workspace.dtype is not torch.uint8 or workspace.get_device() != cache._dev or not workspace.is_contiguous():

@@ -1,8 +1,8 @@
 // A step's rows and pages from the sequences' lengths.  Integer work, bound by the latency of launches and of loads one behind the other; what is read are the
-// tables' columns, once, and the reference counts, once.  Five kernels, each of which needs all of the one before it: every sequence gives back what it
-// does not need and counts its rows and the columns that lack a page; the counts are summed up, and so are the free pages, in blocks; the free pages
-// that are wanted are listed in order; every sequence takes its own; rows are described.  No result depends on the order of atomics: they count
-// references down and nothing reads them in between.
+// tables' columns, once, and the reference counts, once.  Three kernels, each of which needs all of the one before it: every sequence gives back what it
+// does not need and counts its rows and the columns that lack a page; the free pages become a map of bits; every sequence adds up what those before it
+// want, takes the free pages of these ranks and describes its rows.  Many sequences have a kernel of its own for the sums, many rows one for the rows.  No
+// result depends on the order of atomics: they count references down and nothing reads them in between.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -19,14 +19,19 @@ struct Args {
     int64_t *slots;
     int32_t *positions, *tokens;
     int32_t n_text;
-    int32_t *want, *count, *text; // [batch]: columns that lack a page, rows, text rows; then what those of the sequences before add up to (want, text: [batch + 1])
-    int32_t *want_before, *text_before;
-    int32_t *free_in, *free_all;  // [blocks of pages]: free pages; [1]
-    int32_t *list;                // [n_pages]: free pages in order
-    int32_t blocks;
+    int32_t *want, *count, *text; // [batch]: columns that lack a page, rows, text rows
+    int32_t *want_before, *text_before;   // [batch + 1]: what those of the sequences before add up to
+    uint64_t *free_bits;          // [n_pages / 64]
+    int32_t words;                // of free_bits
+    bool rows_here;               // the sequences' own workgroups describe their rows
 };
 
-constexpr int PAGES = 4096;       // of a block
+// Threads of a workgroup; pages of one that looks for free ones.
+constexpr int N = 256, PAGES = 1024;
+// Up to here every workgroup adds up all sequences' counts itself, above one workgroup does it for all (a launch more).
+constexpr int SUMS_EACH = 1024;
+// Up to so many rows the sequences' own workgroups describe them.
+constexpr int ROWS_EACH = 8192;
 
 // What a sequence does in a step (columns: of text, of summaries).
 struct Step {
@@ -54,25 +59,30 @@ __device__ __forceinline__ Step step_of(const Args &a, int b) {
 }
 __device__ __forceinline__ bool names_page(const Args &a, int entry) { return (unsigned)entry < (unsigned)a.rows.n_pages; }
 
-__device__ __forceinline__ int wave_sum(int x) {
+__device__ __forceinline__ int64_t wave_sum(int64_t x) {
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
     return x;
 }
-// The sum of x over a block of N threads, in all of them.
-template <int N>
-__device__ __forceinline__ int block_sum(int x, int *shared) {
-    x = wave_sum(x);
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = x;
-    __syncthreads();
-    int y = 0;
+// Sums of K numbers over a workgroup, in all threads.
+template <int K>
+__device__ __forceinline__ void block_sums(int64_t (&x)[K], int64_t (*shared)[K]) {
 #pragma unroll
-    for (int w = 0; w < N / 64; ++w) y += shared[w];
+    for (int k = 0; k < K; ++k) x[k] = wave_sum(x[k]);
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int k = 0; k < K; ++k) shared[threadIdx.x >> 6][k] = x[k];
     __syncthreads();
-    return y;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        x[k] = 0;
+#pragma unroll
+        for (int w = 0; w < N / 64; ++w) x[k] += shared[w][k];
+    }
+    __syncthreads();
 }
 // Of the threads before this one; `all`: of all.
-template <int N, class T>
+template <class T>
 __device__ __forceinline__ T block_before(T x, T *shared, T &all) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     T upto = x;
@@ -94,140 +104,180 @@ __device__ __forceinline__ T block_before(T x, T *shared, T &all) {
     return before + upto - x;
 }
 
-__device__ __forceinline__ void give_back(const Args &a, int32_t *entry) {
-    const int page = *entry;
-    if (!names_page(a, page)) return;
-    atomicSub(a.refs + page, 1);
-    *entry = -1;
+// Entries of a table's row, `step` apart, several on their way at once.
+template <class F>
+__device__ __forceinline__ void each_entry(const int32_t *row, int from, int to, F &&f) {
+    constexpr int AT_ONCE = 8;
+    for (int x0 = from + threadIdx.x; x0 < to; x0 += N * AT_ONCE) {
+        int entry[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) entry[i] = row[min(x0 + i * N, to - 1)];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i)
+            if (x0 + i * N < to) f(x0 + i * N, entry[i]);
+    }
 }
 
-__global__ __launch_bounds__(256) void ksa_advance_count_kernel(const Args a) {
-    __shared__ int shared[4];
+__global__ __launch_bounds__(N) void ksa_advance_count_kernel(const Args a) {
+    __shared__ int64_t shared[N / 64][1];
     const int b = blockIdx.x;
     const Step s = step_of(a, b);
     int32_t *const text = a.text_table + (int64_t)b * a.rows.text_cols, *const sums = a.sum_table + (int64_t)b * a.rows.sum_cols;
-    int lacks = 0;
+    int64_t lacks[1] = {0};
     if (s.ok) {
-        for (int x = threadIdx.x; x < (s.ended ? a.rows.text_cols : s.begin); x += 256) give_back(a, text + x);
-        if (s.ended)
-            for (int x = threadIdx.x; x < a.rows.sum_cols; x += 256) give_back(a, sums + x);
-        for (int x = s.t0 + threadIdx.x; x < s.t1; x += 256) lacks += !names_page(a, text[x]);
-        for (int x = s.s0 + threadIdx.x; x < s.s1; x += 256) lacks += !names_page(a, sums[x]);
+        auto give_back = [&](int32_t *row) {
+            return [&a, row](int x, int page) {
+                if (!names_page(a, page)) return;
+                atomicSub(a.refs + page, 1);
+                row[x] = -1;
+            };
+        };
+        each_entry(text, 0, s.ended ? a.rows.text_cols : s.begin, give_back(text));
+        if (s.ended) each_entry(sums, 0, a.rows.sum_cols, give_back(sums));
+        each_entry(text, s.t0, s.t1, [&](int, int page) { lacks[0] += !names_page(a, page); });
+        each_entry(sums, s.s0, s.s1, [&](int, int page) { lacks[0] += !names_page(a, page); });
     }
-    lacks = block_sum<256>(lacks, shared);
-    if (threadIdx.x == 0) a.want[b] = lacks, a.count[b] = s.rows, a.text[b] = s.text, a.start[b] = s.start;
+    block_sums(lacks, shared);
+    if (threadIdx.x == 0) a.want[b] = (int)lacks[0], a.count[b] = s.rows, a.text[b] = s.text, a.start[b] = s.start;
 }
 
-// Block 0: sums over the sequences.  Block 1 + x: free pages of the x-th block of them.
-__global__ __launch_bounds__(1024) void ksa_advance_sum_kernel(const Args a) {
-    __shared__ int64_t shared[16];
-    if (blockIdx.x > 0) {
-        const int64_t first = (int64_t)(blockIdx.x - 1) * PAGES;
-        int n = 0;
+// The free pages as bits; with `sums` also what the sequences before each want and have, by the last workgroup.
+__device__ __forceinline__ int clamped(int64_t x) { return (int)min(x, (int64_t)INT32_MAX); }
+__global__ __launch_bounds__(N) void ksa_advance_free_kernel(const Args a) {
+    const int64_t first = (int64_t)blockIdx.x * PAGES + threadIdx.x;
+    if ((int)blockIdx.x < (a.words + PAGES / 64 - 1) / (PAGES / 64)) {
+        int refs[PAGES / N];
 #pragma unroll
-        for (int x = 0; x < PAGES / 1024; ++x) {
-            const int64_t page = first + x * 1024 + threadIdx.x;
-            n += page < a.rows.n_pages && a.refs[page] == 0;
+        for (int x = 0; x < PAGES / N; ++x) refs[x] = a.refs[min(first + x * N, (int64_t)a.rows.n_pages - 1)];
+#pragma unroll
+        for (int x = 0; x < PAGES / N; ++x) {
+            const int64_t page = first + x * N;
+            const uint64_t bits = __builtin_amdgcn_ballot_w64(page < a.rows.n_pages && refs[x] == 0);
+            if ((threadIdx.x & 63) == 0 && page < a.rows.n_pages) a.free_bits[page / 64] = bits;
         }
-        n = block_sum<1024>(n, reinterpret_cast<int *>(shared));
-        if (threadIdx.x == 0) a.free_in[blockIdx.x - 1] = n;
         return;
     }
+    __shared__ int64_t shared[N / 64];
     int64_t before[3] = {0, 0, 0};
     const int32_t *const from[3] = {a.count, a.want, a.text};
     int32_t *const to[3] = {a.cu, a.want_before, a.text_before};
-    for (int b0 = 0; b0 <= a.rows.batch; b0 += 1024) {
+    for (int b0 = 0; b0 <= a.rows.batch; b0 += N) {
         const int b = b0 + threadIdx.x;
 #pragma unroll
         for (int k = 0; k < 3; ++k) {
             int64_t all;
-            const int64_t mine = before[k] + block_before<1024, int64_t>(b < a.rows.batch ? from[k][b] : 0, shared, all);
-            if (b <= a.rows.batch) to[k][b] = (int32_t)min(mine, (int64_t)INT32_MAX);
+            const int64_t mine = before[k] + block_before<int64_t>(b < a.rows.batch ? from[k][b] : 0, shared, all);
+            if (b <= a.rows.batch) to[k][b] = clamped(mine);
             before[k] += all;
         }
     }
 }
 
-// The free pages of a block of them, behind those of the blocks before, as far as they are wanted.
-__global__ __launch_bounds__(1024) void ksa_advance_list_kernel(const Args a) {
-    __shared__ int shared[16];
-    int before = 0, all = 0;
-    for (int x = threadIdx.x; x < a.blocks; x += 1024) {
-        const int n = a.free_in[x];
-        before += x < (int)blockIdx.x ? n : 0, all += n;
-    }
-    before = block_sum<1024>(before, shared);
-    const int wanted = a.want_before[a.rows.batch];
-    if (blockIdx.x == 0) {
-        all = block_sum<1024>(all, shared);
-        if (threadIdx.x == 0) *a.free_all = all, *a.lacking = max(wanted - all, 0);
-    }
-    if (before >= wanted) return;
-    const int64_t first = (int64_t)blockIdx.x * PAGES + threadIdx.x * (PAGES / 1024);
-    bool is_free[PAGES / 1024];
-    int mine = 0;
-#pragma unroll
-    for (int x = 0; x < PAGES / 1024; ++x) is_free[x] = first + x < a.rows.n_pages && a.refs[first + x] == 0, mine += is_free[x];
-    int in_block;
-    int at = before + block_before<1024, int>(mine, shared, in_block);
-#pragma unroll
-    for (int x = 0; x < PAGES / 1024; ++x)
-        if (is_free[x]) {
-            if (at < wanted) a.list[at] = (int32_t)(first + x);
-            ++at;
-        }
+__device__ __forceinline__ void describe(const Args &a, int row, int aug, int b, int text_before, int held) {
+    const int j = ksa_div(aug, a.rows.by_w), in = aug - j * (a.rows.c + a.rows.m);
+    const RowKind kind = kind_of(a.rows, aug);
+    const Spot spot = spot_of(a.rows, entry_of(a.rows, b, kind));
+    if (a.slots) a.slots[row] = spot.page >= 0 ? ((int64_t)spot.page << a.rows.shift) + spot.slot : -1;
+    if (a.positions) a.positions[row] = j * a.rows.c + min(in, a.rows.c - 1);
+    if (a.tokens) a.tokens[row] = kind.text ? clamped((int64_t)text_before + (kind.idx - held)) : -1 - (in - a.rows.c);
+}
+__device__ __forceinline__ void describe_none(const Args &a, int row) {
+    if (a.slots) a.slots[row] = -1;
+    if (a.positions) a.positions[row] = 0;
+    if (a.tokens) a.tokens[row] = -1;
 }
 
-__global__ __launch_bounds__(256) void ksa_advance_take_kernel(const Args a) {
-    __shared__ int shared[4];
-    const int b = blockIdx.x;
+__global__ __launch_bounds__(N) void ksa_advance_take_kernel(const Args a) {
+    __shared__ int64_t shared[N / 64][5];
+    __shared__ int shared_int[N / 64], run_before[N];
+    const int b = blockIdx.x, batch = a.rows.batch;
+    // free pages in the thread's run of words, and in those before it
+    const int each = (a.words + N - 1) / N, w0 = min((int)threadIdx.x * each, a.words), w1 = min(w0 + each, a.words);
+    int free_here = 0, n_free;
+    for (int w = w0; w < w1; ++w) free_here += __builtin_popcountll(a.free_bits[w]);
+    const int want = a.want[b];
     const Step s = step_of(a, b);
-    if (!s.ok || s.ended) return;
-    int at = a.want_before[b];
-    const int n_free = *a.free_all;
-    auto take = [&](int32_t *table, int from, int to) {
-        for (int x0 = from; x0 < to && at < n_free; x0 += 256) {   // (the same in all threads)
-            const int x = x0 + threadIdx.x, lacks = x < to && !names_page(a, table[x]);
-            int all;
-            const int mine = at + block_before<256, int>(lacks, shared, all);
-            if (lacks && mine < n_free) {
-                const int page = a.list[mine];
-                table[x] = page, a.refs[page] = 1;
-            }
-            at += all;
+    // rows and text of the sequences before, rows and wants of all
+    int rows_before, want_before, text_before, all_rows, all_want;
+    if (batch <= SUMS_EACH) {
+        int64_t x[5] = {0, 0, 0, 0, 0};
+        for (int y = threadIdx.x; y < batch; y += N) {
+            const int rows = a.count[y], want = a.want[y], text = a.text[y];
+            if (y < b) x[0] += rows, x[1] += want, x[2] += text;
+            x[3] += rows, x[4] += want;
         }
-    };
-    take(a.text_table + (int64_t)b * a.rows.text_cols, s.t0, s.t1);
-    take(a.sum_table + (int64_t)b * a.rows.sum_cols, s.s0, s.s1);
+        block_sums(x, shared);
+        rows_before = clamped(x[0]), want_before = clamped(x[1]), text_before = clamped(x[2]), all_rows = clamped(x[3]), all_want = clamped(x[4]);
+        if (threadIdx.x == 0) {
+            a.cu[b] = rows_before, a.text_before[b] = text_before;
+            if (b == 0) a.cu[batch] = all_rows;
+        }
+    } else {
+        rows_before = a.cu[b], want_before = a.want_before[b], text_before = a.text_before[b], all_rows = a.cu[batch], all_want = a.want_before[batch];
+    }
+    run_before[threadIdx.x] = block_before<int>(free_here, shared_int, n_free);
+    __syncthreads();
+    if (b == 0 && threadIdx.x == 0) *a.lacking = max(all_want - n_free, 0);
+    const int end = min(want_before + want, n_free);
+    if (end > want_before) {   // (the same in all threads)
+        // the page of a rank: the run of words that holds it, the word, the bit
+        auto page_of = [&](int rank) {
+            int lo = 0, hi = N;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (run_before[mid] <= rank) lo = mid;
+                else hi = mid;
+            }
+            int left = rank - run_before[lo], w = lo * each;
+            uint64_t bits = a.free_bits[w];
+            for (int n = __builtin_popcountll(bits); left >= n; n = __builtin_popcountll(bits)) left -= n, bits = a.free_bits[++w];
+            int at = 0;
+#pragma unroll
+            for (int half = 32; half > 0; half >>= 1) {
+                const int n = __builtin_popcountll(bits >> at & ((1ull << half) - 1));
+                if (left >= n) left -= n, at += half;
+            }
+            return w * 64 + at;
+        };
+        int at = want_before;
+        auto take = [&](int32_t *table, int from, int to) {
+            for (int x0 = from; x0 < to && at < end; x0 += N) {   // (the same in all threads)
+                const int x = x0 + threadIdx.x, lacks = x < to && !names_page(a, table[x]);
+                int all;
+                const int mine = at + block_before<int>(lacks, shared_int, all);
+                if (lacks && mine < end) {
+                    const int page = page_of(mine);
+                    table[x] = page, a.refs[page] = 1;
+                }
+                at += all;
+            }
+        };
+        take(a.text_table + (int64_t)b * a.rows.text_cols, s.t0, s.t1);
+        take(a.sum_table + (int64_t)b * a.rows.sum_cols, s.s0, s.s1);
+        __syncthreads();
+    }
+    if (!a.rows_here) return;
+    const int held = a.held[b];
+    for (int x = threadIdx.x; x < s.rows && rows_before + x < a.rows.total; x += N) describe(a, rows_before + x, s.start + x, b, text_before, held);
+    for (int64_t row = (int64_t)all_rows + b * N + threadIdx.x; row < a.rows.total; row += (int64_t)batch * N) describe_none(a, (int)row);
 }
 
-__global__ __launch_bounds__(256) void ksa_advance_rows_kernel(const Args a) {
-    const int row = blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(N) void ksa_advance_rows_kernel(const Args a) {
+    const int row = blockIdx.x * N + threadIdx.x;
     if (row >= a.rows.total) return;
-    int64_t slot = -1;
-    int position = 0, token = -1;
-    if (row < a.cu[a.rows.batch]) {
-        int lo = 0, hi = a.rows.batch;   // the last sequence that begins at or in front of the row
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (a.cu[mid] <= row) lo = mid;
-            else hi = mid;
-        }
-        const int b = lo, aug = a.start[b] + (row - a.cu[b]), j = ksa_div(aug, a.rows.by_w), in = aug - j * (a.rows.c + a.rows.m);
-        const RowKind kind = kind_of(a.rows, aug);
-        const Spot spot = spot_of(a.rows, entry_of(a.rows, b, kind));
-        if (spot.page >= 0) slot = ((int64_t)spot.page << a.rows.shift) + spot.slot;
-        position = j * a.rows.c + min(in, a.rows.c - 1);
-        token = kind.text ? (int)min((int64_t)a.text_before[b] + (kind.idx - a.held[b]), (int64_t)INT32_MAX) : -1 - (in - a.rows.c);
+    if (row >= a.cu[a.rows.batch]) return describe_none(a, row);
+    int lo = 0, hi = a.rows.batch;   // the last sequence that begins at or in front of the row
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (a.cu[mid] <= row) lo = mid;
+        else hi = mid;
     }
-    if (a.slots) a.slots[row] = slot;
-    if (a.positions) a.positions[row] = position;
-    if (a.tokens) a.tokens[row] = token;
+    describe(a, row, a.start[lo] + (row - a.cu[lo]), lo, a.text_before[lo], a.held[lo]);
 }
 
 }  // namespace
 
-size_t ksa_paged_advance_ints(int32_t batch, int32_t n_pages) { return 5 * (size_t)batch + 2 + ((size_t)n_pages + PAGES - 1) / PAGES + 1 + (size_t)n_pages; }
+size_t ksa_paged_advance_ints(int32_t batch, int32_t n_pages) { return 5 * (size_t)batch + 2 + 2 * (((size_t)n_pages + 63) / 64); }
 
 int ksa_launch_paged_advance(const KsaPagedAdvance &L, void *stream) {
     Args a;
@@ -239,20 +289,22 @@ int ksa_launch_paged_advance(const KsaPagedAdvance &L, void *stream) {
     a.slots = L.slots, a.positions = L.positions, a.tokens = L.tokens;
     a.n_text = L.call.p.n_text;
     const int batch = a.rows.batch;
-    a.blocks = (int)(((int64_t)a.rows.n_pages + PAGES - 1) / PAGES);
+    a.words = (int)(((int64_t)a.rows.n_pages + 63) / 64);
     int32_t *w = L.workspace;
     auto room = [&](int64_t n) {
         int32_t *const at = w;
         w += n;
         return at;
     };
+    a.free_bits = reinterpret_cast<uint64_t *>(room(2 * (int64_t)a.words));   // (first: on 8 bytes)
     a.want = room(batch), a.count = room(batch), a.text = room(batch), a.want_before = room(batch + 1), a.text_before = room(batch + 1);
-    a.free_in = room(a.blocks), a.free_all = room(1), a.list = room(a.rows.n_pages);
+    const bool maps = a.rows.total > 0 && (a.slots || a.positions || a.tokens);
+    a.rows_here = maps && a.rows.total <= ROWS_EACH;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(ksa_advance_count_kernel, dim3(batch), dim3(256), 0, st, a);
-    hipLaunchKernelGGL(ksa_advance_sum_kernel, dim3(1 + a.blocks), dim3(1024), 0, st, a);
-    hipLaunchKernelGGL(ksa_advance_list_kernel, dim3(a.blocks), dim3(1024), 0, st, a);
-    hipLaunchKernelGGL(ksa_advance_take_kernel, dim3(batch), dim3(256), 0, st, a);
-    if (a.rows.total > 0 && (a.slots || a.positions || a.tokens)) hipLaunchKernelGGL(ksa_advance_rows_kernel, dim3((a.rows.total + 255) / 256), dim3(256), 0, st, a);
+    const int blocks = (a.words + PAGES / 64 - 1) / (PAGES / 64);
+    hipLaunchKernelGGL(ksa_advance_count_kernel, dim3(batch), dim3(N), 0, st, a);
+    hipLaunchKernelGGL(ksa_advance_free_kernel, dim3(batch > SUMS_EACH ? blocks + 1 : blocks), dim3(N), 0, st, a);
+    hipLaunchKernelGGL(ksa_advance_take_kernel, dim3(batch), dim3(N), 0, st, a);
+    if (maps && !a.rows_here) hipLaunchKernelGGL(ksa_advance_rows_kernel, dim3((unsigned)(((int64_t)a.rows.total + N - 1) / N)), dim3(N), 0, st, a);
     return hipGetLastError() == hipSuccess ? KSA_OK : KSA_ERR_HIP;
 }
