@@ -486,7 +486,8 @@ int ksa_paged_rotary(const ksa_params *params /*host*/, const ksa_paged_cache *c
  *   Row maps of the step's rows, device [total_rows], each may be NULL: slots (int64): page * page_rows + slot, -1 without a page; positions (int32): as rotary
  *   positions take them; tokens (int32): the row's place among the new text tokens of all sequences, or -1 - s for the s-th summary of its chunk.  Rows behind the last
  *   sequence's get -1, 0 and -1.  total_rows may be less than the rows there are; it only says how long the maps are.
- *   workspace: device, 16-byte aligned, at least ksa_paged_advance_workspace_bytes bytes, needed until the work enqueued on `stream` has finished.
+ *   workspace: device, 16-byte aligned, at least ksa_paged_advance_workspace_bytes bytes, needed until the work enqueued on `stream` has finished;
+ *   calls that share one must be stream-ordered.
  * Counts beyond 2^31 - 1 (cu_rows) stay there.  Nothing is allocated, cleared or waited for; the call may be captured into a graph.  Results do not depend on the
  * order of execution.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^31 columns of
  * both tables over all sequences, or rows, and more), HIP.

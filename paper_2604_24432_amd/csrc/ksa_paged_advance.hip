@@ -1,8 +1,10 @@
 // A step's rows and pages from the sequences' lengths.  Integer work, bound by the latency of launches and of loads one behind the other; what is read are the
 // tables' columns, once, and the reference counts, once.  Three kernels, each of which needs all of the one before it: every sequence gives back what it
 // does not need and counts its rows and the columns that lack a page; the free pages become a map of bits; every sequence adds up what those before it
-// want, takes the free pages of these ranks and describes its rows.  Many sequences have a kernel of its own for the sums, many rows one for the rows.  No
-// result depends on the order of atomics: they count references down and nothing reads them in between.
+// want, takes the free pages of these ranks and describes its rows.  Many rows have a kernel of their own.  No
+// result depends on the order of atomics: they count references down and nothing reads them in between.  64 sequences of 2300 columns, one token each,
+// 13000 pages 4.1, 2.1 and 6.3 us; 200 sequences, 278000 rows, 12000 pages taken of 24000 4.8, 3.0, 9.0 and 5.4.  As five kernels, with sums and a list of the free pages of their own,
+// 22 and 27 us for both; with the list written bit by bit by a thread per run of words the third kernel took 18.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -28,9 +30,9 @@ struct Args {
 
 // Threads of a workgroup; pages of one that looks for free ones.
 constexpr int N = 256, PAGES = 1024;
-// Up to here every workgroup adds up all sequences' counts itself, above one workgroup does it for all (a launch more).
+// Up to here every workgroup adds up all sequences' counts itself (12 KB of them at most), above one workgroup does it for all, beside those that look for free pages.
 constexpr int SUMS_EACH = 1024;
-// Up to so many rows the sequences' own workgroups describe them.
+// Up to so many rows the sequences' own workgroups describe them (all of one sequence: 32 passes), above a launch more does.
 constexpr int ROWS_EACH = 8192;
 
 // What a sequence does in a step (columns: of text, of summaries).
@@ -141,7 +143,7 @@ __global__ __launch_bounds__(N) void ksa_advance_count_kernel(const Args a) {
     if (threadIdx.x == 0) a.want[b] = (int)lacks[0], a.count[b] = s.rows, a.text[b] = s.text, a.start[b] = s.start;
 }
 
-// The free pages as bits; with `sums` also what the sequences before each want and have, by the last workgroup.
+// The free pages as bits; of many sequences also what those before each of them want and have, by the last workgroup.
 __device__ __forceinline__ int clamped(int64_t x) { return (int)min(x, (int64_t)INT32_MAX); }
 __global__ __launch_bounds__(N) void ksa_advance_free_kernel(const Args a) {
     const int64_t first = (int64_t)blockIdx.x * PAGES + threadIdx.x;

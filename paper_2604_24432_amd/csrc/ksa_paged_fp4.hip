@@ -9,6 +9,13 @@ namespace {
 //     exponent, are its operands of four products one after the other.  K goes through the conversion to bf16 (exact) but not through LDS.
 //   - With at most 16 pairs the products have 16 columns: half the weights, half the products' time and half the accumulators of 32.
 //   - V is converted where it was loaded, goes through LDS as bf16 and comes back transposed; K's rows are V's, so that an entry is looked up once.
+// 64 sequences at 128K, 32/8 heads, 1.15 GB: 170 us, 6.7 TB/s (through the kernel of the other formats 277), of the 6.5 - 6.8 that a plain read reaches; the
+// vector unit issues 72 % of the time, 227 instructions per block. 16 sequences of 1 .. 8 rows, 32 columns, 100 MB: 34 us in four spans; there the matrix unit's time and the vector
+// instructions' (237 per block) add up to 90 % of it. One of 700 keys 4.9 us. Dropped (us, before and after): one scalar address for keys side by side in a page
+// (128K 198, 206), two blocks on their way (16 columns have no registers for them: 181, 315; 32 columns level), operands of V read ahead of the weights (level), 64 keys
+// per block for 32 columns (32 x 8 rows at 128K 124, 121; the 16 sequences 34.8, 36), two workgroups of 16 columns for 32 pairs (127, 176), loads that stay in the
+// caches (128K 182, 200). Products of 4-bit K with q in two 8-bit parts, which need no conversion, are exact one by one, but the matrix unit's sums of them are not: off by
+// 2^-18 of the terms' sizes, by 2^-13 where q's elements are 2^10 apart.
 template <int COLS>
 struct Acc;
 template <>
@@ -54,7 +61,7 @@ __global__ __launch_bounds__(WAVES * 64, COLS == 16 || D == 64 ? 4 : 2) void ksa
     constexpr int WORDS = BYTES / 4, PIECES = BYTES / 16 < 1 ? 1 : BYTES / 16, EACH = WORDS / PIECES;   // pieces of EACH words of one group
     constexpr int KS = WORDS, TILES = ROWS;             // products per tile of COLS keys, tiles of a block
     constexpr int AB = D / COLS, PER = COLS == 16 ? 4 : 16;   // blocks of columns of the output, values of a product per lane
-    constexpr int VROW = D * 2 + 48;                    // bytes: fewest bank conflicts of writes and transposing reads
+    constexpr int VROW = D * 2 + 48;                    // bytes: conflicts are 25 % of the LDS cycles of 32 columns, with 32 more bytes 49 %, with 64 66 %
     constexpr int OWN = BLOCK * VROW, PARTS = COLS / 16, PART = D / PARTS, OUT_ROW = PART + 4;   // the results pass through the blocks' memory, in parts of the columns
     static_assert(COLS * OUT_ROW * 4 <= OWN, "a part of a wave's results lies where its blocks were");
     __shared__ __align__(16) unsigned char lds[WAVES * OWN];

@@ -476,7 +476,8 @@ template <int D, int F, int NW, int GROUPS>
 __global__ __launch_bounds__(NW * GROUPS * 64, 2) void ksa_paged_many_kernel(const FwdArgs a) {
     constexpr int KS = D / 16, DB = D / 32, PAIRS = NW * 32;
     constexpr int RW = BN / NW;                                       // rows of a tile that a wave fetches
-    constexpr int EACH = is_fp4(F) ? D / (2 * NW) : 16;               // bytes of a row per lane and load; a wave's rows of 4 bits are one load
+    // bytes of a row per lane and load; a wave's rows of 4 bits are one load (with 16 bytes half of the lanes would repeat the others': 4608 rows at 128K 1175 us, now 1033 - 1060)
+    constexpr int EACH = is_fp4(F) ? D / (2 * NW) : 16;
     constexpr int LPR = bytes_of(F, D) / EACH, RPI = 64 / LPR < RW ? 64 / LPR : RW, NI = RW / RPI;   // lanes per row, rows per load, loads per wave and tensor
     constexpr int AS_BF16 = EACH * 2 * D / bytes_of(F, D);            // what they are as bf16
     typedef unsigned piece_t __attribute__((ext_vector_type(EACH / 4)));

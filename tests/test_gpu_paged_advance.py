@@ -275,3 +275,32 @@ def test_python_refuses_what_does_not_fit():
     with pytest.raises(K.KsaError):
         K.ksa_paged_advance(*good, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert bits(torch.zeros(1, dtype=torch.bfloat16)).item() == 0
+
+
+def test_two_graphs_share_a_workspace():
+    """Two batches' steps captured with one workspace, replayed in turn: each as alone."""
+    say("advance two graphs")
+    a, b = Books(5, 300, 16, 2, 1, 16, 60), Books(9, 500, 64, 8, 1, 32, 200)
+    ws = torch.empty(max(K.paged_advance_workspace_bytes(x.cache) for x in (a, b)), dtype=torch.uint8, device="cuda")
+    made = []
+    for books, total in ((a, 100), (b, 300)):
+        n = len(books.text)
+        held, new = books.dev([0] * n), books.dev([0] * n)
+        step = K.ksa_paged_advance(books.cache, books.refs_dev, held, new, total, workspace=ws)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            K.ksa_paged_advance(books.cache, books.refs_dev, held, new, total, step=step, workspace=ws)
+        made.append((books, total, held, new, step, graph, [0] * n))
+    g = random.Random(8)
+    for _ in range(6):
+        wants = []
+        for books, total, held, new, step, graph, lengths in made:
+            t = [min(g.choice([0, 1, g.randint(1, 60)]), books.shape[4] - h) for h in lengths]
+            held.copy_(books.dev(lengths)), new.copy_(books.dev(t))
+            wants.append(advance(*books.shape, books.text, books.sums, books.refs, lengths, t))
+            lengths[:] = [h + x for h, x in zip(lengths, t)]
+        for books, total, held, new, step, graph, lengths in made:
+            graph.replay()
+        torch.cuda.synchronize()
+        for (books, total, held, new, step, graph, lengths), want in zip(made, wants):
+            books.check(step, want, total)

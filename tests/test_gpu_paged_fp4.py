@@ -358,3 +358,60 @@ def test_python_refuses_what_does_not_fit():
                 (k, k, text, sums, e[..., 0], e[..., 0]), (k, k.to(torch.bfloat16), text, sums, e, e), (k, k, text, sums, e.int(), e.int())):
         with pytest.raises(ValueError):
             K.PagedCache(p, *bad)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [1, 5])
+def test_more_workgroups_than_places(d, rows):
+    """Beyond 512 workgroups of few rows, where those of four waves take over; 16 and 32 columns of pairs, sequences of many lengths, some without rows."""
+    say(f"fp4 many workgroups d={d} rows={rows}")
+    B = 140
+    p = K.make_params(B, 1024, 16, 2, 3, 16, 4, d)
+    first, count = [(37 * b) % 190 for b in range(B)], [rows if b % 7 else b % 2 for b in range(B)]
+    for n_splits in (1, 2):
+        check_attention(p, 16, first, count, 41, n_splits, rows)
+
+
+@pytest.mark.parametrize("rows", [1, 4, 70])
+@pytest.mark.parametrize("n_splits", [1, 2])
+def test_sequences_out_of_place(rows, n_splits):
+    """A sequence that starts outside the text, has more rows than were said, or borders outside the tensor: NaN for its rows, the others as they were."""
+    say(f"fp4 out of place rows={rows} splits={n_splits}")
+    p = K.make_params(4, 300, 16, 2, 2, 8, 2, 128)
+    pages = Pages4(p, [200] * 4, 16, 3)
+    for b in range(4):
+        pages.put(b, 0, randn(200, 2, 128, seed=b), randn(200, 2, 128, seed=b + 9))
+    total = 4 * rows
+    q = randn(total + 3, 8, 128, seed=5)
+    cu = torch.arange(5, dtype=torch.int32, device="cuda") * rows
+    start = torch.full((4,), 100, dtype=torch.int32, device="cuda")
+
+    def run(cu, start, max_rows=rows):
+        o, lse = torch.full_like(q, 7.0), torch.full((total + 3, 8), 7.0, device="cuda")
+        K.ksa_paged_fwd(pages.cache, q, cu, start, max_rows=max_rows, o=o, lse=lse, n_splits=n_splits)
+        return o, lse
+
+    good = run(cu, start)
+    assert bool(torch.isfinite(good[0][:total].float()).all()) and bool((good[0][total:] == 7).all()) and bool((good[1][total:] == 7).all())
+    for bad in (-1, 10 ** 6, 338 - rows + 1):                              # 300 text tokens have 336 rows
+        at = start.clone()
+        at[2] = bad
+        for got, want in zip(run(cu, at), good):
+            assert bool(torch.isnan(got[2 * rows:3 * rows]).all())
+            assert torch.equal(got[:2 * rows], want[:2 * rows]) and torch.equal(got[3 * rows:], want[3 * rows:])
+
+
+def test_a_stream_of_its_own():
+    say("fp4 stream")
+    p = K.make_params(2, 2048, 16, 2, 3, 8, 2, 128)
+    pages = Pages4(p, [900, 900], 16, 3)
+    k, v, q = randn(1800, 2, 128, seed=1), randn(1800, 2, 128, seed=2), randn(2, 8, 128, seed=3)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    K.ksa_paged_append(pages.cache, k, v, *batch_of([0, 0], [900, 900]), stream=stream)
+    o, lse = K.ksa_paged_fwd(pages.cache, q, *batch_of([899, 899], [1, 1]), max_rows=1, stream=stream)
+    kb, _ = K.ksa_paged_read(pages.cache, *batch_of([0, 0], [900, 900]), 1800, stream=stream)
+    stream.synchronize()
+    assert torch.equal(kb.double(), e2m1(k.double())[0])
+    o1, lse1 = K.ksa_paged_fwd(pages.cache, q, *batch_of([899, 899], [1, 1]), max_rows=1)
+    assert torch.equal(bits(o), bits(o1)) and torch.equal(lse, lse1)

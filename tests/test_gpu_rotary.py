@@ -252,3 +252,64 @@ def test_python_refuses_what_does_not_fit():
     for bad in ((x, y, y[:4], cu, start), (x[:4], y, y, cu, start), (x, y, y, cu[:1], start), (x, y, y, cu.long(), start), (None, y, y, cu, start, x), (y, y, y, cu, start)):
         with pytest.raises(ValueError):
             K.ksa_paged_rotary(pages.cache, r, *bad)
+
+
+def test_rows_further_apart_than_32_bits():
+    say("rotary far rows")
+    p = K.make_params(2, 40, 16, 2, 1, 3, 1, 64)
+    L = K.binding.augmented_rows(p, 40)
+    far = torch.empty(6 << 30, dtype=torch.uint8, device="cuda").view(torch.bfloat16)          # 3 Gi elements
+    row = (3 << 30) // (2 * L + 1) // 8 * 8
+    q = torch.as_strided(far, (2, L, 3, 64), (L * row, row, 64, 1))
+    x = randn(2, L, 3, 64, seed=1)
+    q.copy_(x)
+    r = handle(dict(dim=64))
+    out, _ = K.ksa_rotary_fwd(p, r, q, None, torch.empty_like(x))
+    at = positions(range(L), 16, 2)
+    within(out, x, dict(dim=64), at)
+    K.ksa_rotary_fwd(p, r, q, None, q)
+    assert torch.equal(bits(q), bits(out))
+    pages = Pages(p, [L, L], 16, False, 5, fill=0.0)
+    q.copy_(x)
+    k = torch.as_strided(far, (2 * L, 1, 64), (row, 64, 1), 192)                               # behind the heads of q
+    k.copy_(x[:, :, :1].flatten(0, 1))
+    cu, start = batch_of([0, 0], [L, L])
+    got = K.ksa_paged_rotary(pages.cache, r, torch.as_strided(far, (2 * L, 3, 64), (row, 64, 1)), k, k, cu, start, q_out=torch.empty_like(x).view(2 * L, 3, 64))
+    assert torch.equal(bits(got.view_as(out)), bits(out))
+    kb, vb = K.ksa_paged_read(pages.cache, cu, start, 2 * L)
+    assert torch.equal(bits(kb.view(2, L, 1, 64)), bits(out[:, :, :1])) and torch.equal(bits(vb), bits(k.contiguous()))
+
+
+def test_what_training_does_beside_captured_steps():
+    """Forward, attention and backward through turned q and k: gradients of a whole layer's scores against float64 autograd of the definition."""
+    say("rotary with prefill")
+    p = K.make_params(1, 48, 16, 2, 1, 4, 2, 64)
+    lay = K.Layout(p)
+    L = lay.aug_len
+    rule = dict(dim=32, base=500.0, scaling="by_parts", factor=2.0, original=64.0)
+    r = handle(rule)
+    q, k, v, g = (randn(1, L, h, 64, seed=s) * 0.5 for h, s in ((4, 1), (2, 2), (2, 3), (4, 4)))
+    qt, kt = K.ksa_rotary_fwd(p, r, q, k)
+    o, lse = K.ksa_prefill_fwd(lay, qt, kt, v)
+    dqt, dkt, dv = K.ksa_prefill_bwd(lay, qt, kt, v, o, lse, g)
+    dq, dk = K.ksa_rotary_bwd(p, r, dqt, dkt)
+    see = torch.from_numpy(np.stack([lay.mask_row(i) for i in range(L)])).bool()
+    at = positions(range(L), 16, 2)
+    x = [t[0].double().cpu().requires_grad_() for t in (q, k, v)]
+
+    def plain(y):      # the definition again, in operations that autograd can follow
+        from tests.rotary import frequencies
+        f, magnitude = frequencies(rule)
+        angle = torch.tensor(at, dtype=torch.float64)[:, None, None] * torch.tensor(f, dtype=torch.float64)
+        a, b = y[..., :16], y[..., 16:32]
+        return torch.cat([(a * angle.cos() - b * angle.sin()) * magnitude, (b * angle.cos() + a * angle.sin()) * magnitude, y[..., 32:]], -1)
+    qd, kd = plain(x[0]), plain(x[1])
+    out = []
+    for h in range(4):
+        s = (qd[:, h] @ kd[:, h // 2].T / 8).masked_fill(~see, -math.inf)
+        out.append(torch.softmax(s, 1) @ x[2][:, h // 2])
+    torch.stack(out, 1).backward(g[0].double().cpu())
+    # the bars of the prefill's own gradients (2e-2 + 2^-8 of the entry), turned: a pair's entries share theirs, times the magnitude, and one more rounding
+    for got, want in ((dq, x[0].grad), (dk, x[1].grad), (dv, x[2].grad)):
+        err = (got[0].double().cpu() - want).abs()
+        assert bool((err <= 2 * 1.07 * 2e-2 + 2.0 ** -7 * want.abs()).all()) and float(err.mean()) <= 2 * 2e-3, float(err.max())
