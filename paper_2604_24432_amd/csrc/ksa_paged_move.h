@@ -144,7 +144,13 @@ __global__ __launch_bounds__(256) void ksa_paged_append_kernel(const MoveArgs a)
     if (p.page < 0) return;
     const int piece = threadIdx.x % LANES;
     const int64_t from = p.row * a.row_stride + p.head * a.head_stride + piece * 8;
-    const u32x4 k = *reinterpret_cast<const u32x4 *>(a.k + from), v = *reinterpret_cast<const u32x4 *>(a.v + from);
+    // (4 bits: what is read is four times what is written, and is not kept in the caches: 36864 rows in and out 75.0 us -> 72.0)
+    auto load = [](const __bf16 *x) {
+        const u32x4 *const at = reinterpret_cast<const u32x4 *>(x);
+        if constexpr (F == KSA_CACHE_FP4) return __builtin_nontemporal_load(at);
+        else return *at;
+    };
+    const u32x4 k = load(a.k + from), v = load(a.v + from);
     put_piece<D, F>(a, p, piece, k, v);
 }
 
