@@ -1,7 +1,7 @@
 // Rows into and out of the paged cache, as bf16, as e4m3 numbers with one power of two per row and KV head, or as e2m1 numbers with one per 32 of them.  Data movement, bound by
 // HBM: 16 bytes of a row per lane, the row's largest magnitude by lane moves, the table looked up by every row's lanes.  36864 rows, 8 heads,
 // d 128, 8-bit: in 56 us and out again 34, 454 MB at 5.0 TB/s (a copy on this card 5.0); 54000 rows, 16 heads, bf16, out 100 us, 5.3 TB/s; the 36864 rows in 4 bits
-// in 44 us, 4.4 TB/s, and out again 30; 64 rows
+// in 42 us, 4.5 TB/s, and out again 30; 64 rows
 // of 64 sequences 2.8 us, a launch and three loads one behind the other.  Loads of the new rows in front of the lookup (in 61 / 3.3 us),
 // two or four rows per lane (66 / 3.9, 69 / 5.0) did not pay.
 #ifndef KSA_PAGED_MOVE_H_

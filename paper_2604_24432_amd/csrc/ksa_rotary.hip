@@ -1,6 +1,6 @@
 // Rotary positions of whole augmented sequences, there and back.  Data movement, bound by HBM: a wave has a row, or a part of its heads; its lanes work out
 // the row's cosines and sines, one pair each, share them in LDS and then go over the heads, 16 bytes of one per lane and the 16 that they are paired with (from the
-// cache: the same lines).  36864 rows, 40 heads of 128, 755 MB: 138 us, 5.5 TB/s (a copy on this card 5.0); 12022 rows, 16 heads of 64 11.3 us, 4.9; 100 rows 3.
+// cache: the same lines).  36864 rows, 40 heads of 128, 755 MB: 130 us, 5.8 TB/s (a copy on this card 5.0); 12022 rows, 16 heads of 64 11.3 us, 4.9; 100 rows 3.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -22,7 +22,11 @@ struct Args {
     int32_t w;
 };
 
-template <int D, int P>
+// Outputs of this many bytes and more, which the caches (256 MB behind the L2s) cannot keep for whoever reads them next, go past them: 36864 rows, 40 heads of 128, 378 MB
+// there and back 272 us -> 261. Below, the next kernel finds them there.
+constexpr int64_t PAST_CACHES = (int64_t)256 << 20;
+
+template <int D, int P, bool PAST>
 __global__ __launch_bounds__(256) void ksa_rotary_kernel(const Args a) {
     constexpr int LANES = D / 8, PER = 64 / LANES, AT_ONCE = 4;   // lanes of a head, heads of a wave's access, accesses on their way
     __shared__ __align__(16) float table[4][64][2];
@@ -47,17 +51,25 @@ __global__ __launch_bounds__(256) void ksa_rotary_kernel(const Args a) {
             const int h = h0 + i * step, of = h >= a.heads[0] ? 1 : 0, head = h - (of ? a.heads[0] : 0);
             if (h >= all) break;
             __bf16 *const to = of ? a.out[1] + b * a.out_batch[1] + at * a.out_row[1] + head * a.out_head[1] : a.out[0] + b * a.out_batch[0] + at * a.out_row[0] + head * a.out_head[0];
-            *reinterpret_cast<u32x4 *>(to + piece * 8) = turned<P>(a.rotary, x[i], piece, t);
+            u32x4 *const at_piece = reinterpret_cast<u32x4 *>(to + piece * 8);
+            const u32x4 y = turned<P>(a.rotary, x[i], piece, t);
+            if constexpr (PAST) __builtin_nontemporal_store(y, at_piece);
+            else *at_piece = y;
         }
     }
 }
 
+template <int D, int P>
+void launch(const Args &a, hipStream_t st) {
+    const dim3 grid((unsigned)((a.units + 3) / 4));
+    if ((int64_t)a.units / a.parts * (a.heads[0] + a.heads[1]) * D * 2 >= PAST_CACHES) hipLaunchKernelGGL((ksa_rotary_kernel<D, P, true>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((ksa_rotary_kernel<D, P, false>), grid, dim3(256), 0, st, a);
+}
 template <int D>
 void launch(const Args &a, int pairs, hipStream_t st) {
-    const dim3 grid((unsigned)((a.units + 3) / 4));
-    if (pairs == KSA_HALF) hipLaunchKernelGGL((ksa_rotary_kernel<D, KSA_HALF>), grid, dim3(256), 0, st, a);
-    else if (pairs == KSA_NEXT) hipLaunchKernelGGL((ksa_rotary_kernel<D, KSA_NEXT>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((ksa_rotary_kernel<D, KSA_HALF_ANY>), grid, dim3(256), 0, st, a);
+    if (pairs == KSA_HALF) launch<D, KSA_HALF>(a, st);
+    else if (pairs == KSA_NEXT) launch<D, KSA_NEXT>(a, st);
+    else launch<D, KSA_HALF_ANY>(a, st);
 }
 
 }  // namespace

@@ -12,7 +12,7 @@ from tests.test_codegen import _assembly, _kernels
 # source: kernel -> instantiations
 KERNELS = {"ksa_paged_fp4.hip": {"ksa_paged_few_fp4_kernel": 6, "ksa_paged_many_kernel": 6},
            "ksa_paged_cache_fp4.hip": {"ksa_paged_append_kernel": 2, "ksa_paged_read_kernel": 2},
-           "ksa_rotary.hip": {"ksa_rotary_kernel": 6}, "ksa_paged_rotary.hip": {"ksa_paged_rotary_kernel": 18},
+           "ksa_rotary.hip": {"ksa_rotary_kernel": 12}, "ksa_paged_rotary.hip": {"ksa_paged_rotary_kernel": 18},
            "ksa_paged_advance.hip": {"ksa_advance_count_kernel": 1, "ksa_advance_free_kernel": 1, "ksa_advance_take_kernel": 1, "ksa_advance_rows_kernel": 1}}
 
 

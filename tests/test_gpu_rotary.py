@@ -313,3 +313,25 @@ def test_what_training_does_beside_captured_steps():
     for got, want in ((dq, x[0].grad), (dk, x[1].grad), (dv, x[2].grad)):
         err = (got[0].double().cpu() - want).abs()
         assert bool((err <= 2 * 1.07 * 2e-2 + 2.0 ** -7 * want.abs()).all()) and float(err.mean()) <= 2 * 2e-3, float(err.max())
+
+
+@pytest.mark.parametrize("rule", [dict(dim=128), dict(dim=64, interleaved=True), dict(dim=36)], ids=name)
+def test_outputs_larger_than_the_caches(rule):
+    """From 256 MB of output on another kernel runs: the same bits as the sequence's beginning alone, and the definition at its end; in place too."""
+    say(f"rotary large {rule}")
+    c, m, n = 64, 8, 60000
+    p, few = K.make_params(1, n, c, m, 1, 16, 2, 128), K.make_params(1, 1000, c, m, 1, 16, 2, 128)
+    L, L0 = K.binding.augmented_rows(p, n), K.binding.augmented_rows(p, 1000)
+    assert L * 18 * 128 * 2 >= 256 << 20 > L0 * 18 * 128 * 2
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, k = (torch.randn(1, L, h, 128, generator=g, device="cuda").to(torch.bfloat16) for h in (16, 2))
+    r = handle(rule)
+    for call, back in ((K.ksa_rotary_fwd, False), (K.ksa_rotary_bwd, True)):
+        got = call(p, r, q, k)
+        for x, y in zip(got, call(few, r, q[:, :L0].contiguous(), k[:, :L0].contiguous())):
+            assert torch.equal(bits(x[:, :L0]), bits(y))
+        for x, y in zip(got, (q, k)):
+            within(x[:, -100:], y[:, -100:], rule, positions(range(L - 100, L), c, m), back)
+    inout = q.clone()
+    K.ksa_rotary_bwd(p, r, inout, None, inout)
+    assert torch.equal(bits(inout), bits(got[0]))
