@@ -600,7 +600,7 @@ __global__ __launch_bounds__(NW * GROUPS * 64, 2) void ksa_paged_many_kernel(con
     // Half y of step t.  SCORES: of keys 32 y .. of K tile t, into sc[y].  WEIGHTS: of sc[y ^ 1] (half 0: tile t - 1, half 1: tile t) into
     // p[y ^ 1].  OUT: V tile t - 1, keys 32 y .., times p[y].  A slot is one MFMA and what the vector unit does beside it, pinned by fences;
     // beside(x) is what slot x of the half does for the tiles on their way.
-    constexpr int AHEAD = 3, AHEAD_V = 2;   // operands are read so many slots before the MFMAs that use them
+    constexpr int AHEAD = is_fp4(F) ? 2 : 3, AHEAD_V = 2;   // operands are read so many slots before the MFMAs that use them (4 bits: three 1 - 2 % slower)
     bf16x8 k[KS];
     auto read_k = [&](int t, int y, int x) { k[x] = *reinterpret_cast<const bf16x8 *>(lds + (t & 1) * K_BYTES + y * 32 * KROW + k_at + x * 32); };
     auto half = [&](int t, auto y_tag, auto scores_tag, auto weights_tag, auto out_tag, auto &&beside) {
