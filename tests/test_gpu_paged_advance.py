@@ -82,13 +82,14 @@ def test_loops_of_steps(case):
     assert n_pages != 24 or ran_out > 0
 
 
-def test_many_sequences_and_many_pages():
-    say("advance large")
+@pytest.mark.parametrize("B,n", [(2500, 3000), (5000, 700)])
+def test_many_sequences_and_many_pages(B, n):
+    """Counts added up by every workgroup, and from 4096 sequences on by one for all."""
+    say(f"advance large {B}")
     g = random.Random(4)
-    B, n = 2500, 3000
     books = Books(B, n, 64, 8, 1, 64, 70001)
     held = [0] * B
-    for most in (3000, 1, 1, 500):
+    for most in (n, 1, 1, n // 6):
         new = [min(g.choice([0, 1, g.randint(1, most), -1 if held[0] else 1]), n - h) for h in held]
         books.step(held, new)
         held = [0 if t < 0 else h + t for h, t in zip(held, new)]
