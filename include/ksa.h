@@ -457,6 +457,14 @@ int ksa_rotary_bwd(const ksa_params *params /*host*/, const ksa_rotary *rotary /
                    const int64_t dq_out_strides[3], const int64_t dk_out_strides[3], const int64_t dq_strides[3], const int64_t dk_strides[3], void *stream);
 
 /*
+ * ksa_rotary_step: one new row per sequence of the decode loop (ksa_decode_fwd, ksa_cache_append): q [B, Hq, d] into q_out, k [B, Hkv, d] into k_out. kind and pos
+ * (device int32 [B]) as in ksa_cache_append: text indices, or summary ordinals. Rows of a sequence whose pos is outside the text (its whole chunks' summaries) become NaN.
+ * *_strides = {batch, head}; all else as ksa_rotary_fwd. Errors also: INVALID_ARG (unknown kind, kind = SUMMARY with m = 0, null or misaligned pos).
+ */
+int ksa_rotary_step(const ksa_params *params /*host*/, const ksa_rotary *rotary /*host*/, int32_t kind, const void *q, const void *k, const int32_t *pos, void *q_out,
+                    void *k_out, const int64_t q_strides[2], const int64_t k_strides[2], const int64_t q_out_strides[2], const int64_t k_out_strides[2], void *stream);
+
+/*
  * ksa_paged_rotary: a serving step's new rows in one launch: q (device bf16 [total_rows, Hq, d]) is turned into q_out, k_new is turned, and goes with v_new into the
  * cache, as ksa_paged_append puts it (k is rounded to bf16 in between: the same bits as in two steps).  Batch, tables, capacity and errors as there (and UNSUPPORTED
  * from 2^26 rows on); rows of q of a sequence out of place become NaN in q_out.  q and q_out may be NULL; q_out may be the memory of q (same strides).

@@ -104,6 +104,7 @@ def lib():
         "ksa_rotary_turns": (C.c_int, [C.POINTER(ksa_rotary_rule), C.POINTER(C.c_uint64), C.POINTER(C.c_float)]),
         "ksa_rotary_fwd": (C.c_int, [pp, vp, vp, vp, vp, vp, i64p, i64p, i64p, i64p, vp]),
         "ksa_rotary_bwd": (C.c_int, [pp, vp, vp, vp, vp, vp, i64p, i64p, i64p, i64p, vp]),
+        "ksa_rotary_step": (C.c_int, [pp, vp, C.c_int32, vp, vp, vp, vp, vp, i64p, i64p, i64p, i64p, vp]),
         "ksa_paged_rotary": (C.c_int, [pp, vp, vp, vp, vp, vp, vp, i64p, i64p, i64p, vp, vp, C.c_int64, vp]),
         "ksa_status_string": (C.c_char_p, [C.c_int]),
         "ksa_build_info": (C.c_char_p, []),
@@ -122,7 +123,7 @@ EXPORTED_SYMBOLS = ("ksa_augmented_rows", "ksa_build_layout", "ksa_layout_destro
                     "ksa_cache_summary_row", "ksa_decode_ranges", "ksa_decode_workspace_bytes",
                     "ksa_decode_fwd", "ksa_decode_fwd_static", "ksa_decode_summary_ranges", "ksa_decode_summary_fwd", "ksa_cache_from_prefill",
                     "ksa_cache_append", "ksa_paged_pages", "ksa_paged_append", "ksa_paged_read", "ksa_paged_workspace_bytes", "ksa_paged_fwd",
-                    "ksa_paged_advance_workspace_bytes", "ksa_paged_advance", "ksa_rotary_turns", "ksa_rotary_fwd", "ksa_rotary_bwd", "ksa_paged_rotary", "ksa_status_string", "ksa_build_info")
+                    "ksa_paged_advance_workspace_bytes", "ksa_paged_advance", "ksa_rotary_turns", "ksa_rotary_fwd", "ksa_rotary_bwd", "ksa_rotary_step", "ksa_paged_rotary", "ksa_status_string", "ksa_build_info")
 
 
 def status_string(status: int) -> str:
@@ -847,6 +848,40 @@ def ksa_rotary_fwd(params: ksa_params, rotary: Rotary, q, k, q_out=None, k_out=N
 def ksa_rotary_bwd(params: ksa_params, rotary: Rotary, dq_out, dk_out, dq=None, dk=None, stream=None):
     """Gradients with respect to ksa_rotary_fwd's outputs -> with respect to its q and k."""
     return _rotary_call("ksa_rotary_bwd", params, rotary, (dq_out, dk_out), (dq, dk), ("dq_out", "dk_out"), stream)
+
+
+def ksa_rotary_step(params: ksa_params, rotary: Rotary, kind: int, q, k, pos, q_out=None, k_out=None, stream=None):
+    """The decode loop's new rows, one per sequence: q [B, Hq, d] and k [B, Hkv, d] bf16 (either may be None) turned by pos int32 [B], text indices or summary
+    ordinals by `kind` (KSA_ROW_TEXT, KSA_ROW_SUMMARY), before ksa_cache_append and ksa_decode_fwd.  An output may be its input."""
+    import torch
+    if q is None and k is None:
+        raise ValueError("q and k are both missing")
+    if stream is not None and (q is not None and q_out is None or k is not None and k_out is None):
+        if stream.device != rotary.device:
+            raise ValueError("stream belongs to another device than the tensors")
+        with torch.cuda.stream(stream):      # what is allocated here belongs to `stream`
+            return ksa_rotary_step(params, rotary, kind, q, k, pos, q_out, k_out)
+    batch, _, _, _, _, _, n_q_heads, n_kv_heads, d = _FIELDS.unpack_from(params)
+    if q is not None and q_out is None:
+        q_out = torch.empty_like(q)
+    if k is not None and k_out is None:
+        k_out = torch.empty_like(k)
+    _require(pos, "pos", torch.int32, 1)
+    if pos.shape[0] != batch or pos.stride(0) != 1 or pos.get_device() != rotary._dev:
+        raise ValueError(f"pos must be {batch} contiguous elements on the frequencies' device")
+    strides = []
+    for x, y, what, shape in ((q, q_out, "q", (batch, n_q_heads, d)), (k, k_out, "k", (batch, n_kv_heads, d))):
+        if x is None and y is not None:
+            raise ValueError(f"an output is given for {what}, which is missing")
+        for t in (x, y):
+            if t is not None:
+                _require(t, what, torch.bfloat16, 3)
+                if t.shape != shape or t.get_device() != rotary._dev:
+                    raise ValueError(f"{what}: expected {shape} on the frequencies' device, got {tuple(t.shape)}")
+            strides.append(None if t is None or t.is_contiguous() else _strides_of(t))
+    _on_device(rotary._dev, "ksa_rotary_step", stream, C.byref(params), rotary._arg, kind, q.data_ptr() if q is not None else None, k.data_ptr() if k is not None else None,
+               pos.data_ptr(), q_out.data_ptr() if q is not None else None, k_out.data_ptr() if k is not None else None, strides[0], strides[2], strides[1], strides[3])
+    return q_out, k_out
 
 
 def ksa_paged_rotary(cache: PagedCache, rotary: Rotary, q, k_new, v_new, cu_rows, start, q_out=None, stream=None):

@@ -6,12 +6,14 @@
 
 #include "ksa.h"
 
-// Whole sequences: q, k and their outputs, any of the pairs null.  Strides {batch, row, head} in elements.
+// Whole sequences, or (pos) one row of each: q, k and their outputs, any of the pairs null.  Strides {batch, row, head} in elements.
 struct KsaRotaryCall {
     ksa_params p;
     ksa_rotary rotary;
-    int32_t aug_len;
+    int32_t rows;                 // of a sequence
     bool back;                    // turned back
+    const int32_t *pos;           // the rows' text indices, or summary ordinals
+    int32_t kind;                 // KSA_ROW_*
     const void *in[2];            // q, k
     void *out[2];
     int64_t in_strides[2][3], out_strides[2][3];

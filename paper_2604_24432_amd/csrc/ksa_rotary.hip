@@ -1,4 +1,4 @@
-// Rotary positions of whole augmented sequences, there and back.  Data movement, bound by HBM: a wave has a row, or a part of its heads; its lanes work out
+// Rotary positions of whole augmented sequences, there and back, and of one row of each.  Data movement, bound by HBM: a wave has a row, or a part of its heads; its lanes work out
 // the row's cosines and sines, one pair each, share them in LDS and then go over the heads, 16 bytes of one per lane and the 16 that they are paired with (from the
 // cache: the same lines).  36864 rows, 40 heads of 128, 755 MB: 130 us, 5.8 TB/s (a copy on this card 5.0); 12022 rows, 16 heads of 64 11.3 us, 4.9; 100 rows 3.
 #include <hip/hip_runtime.h>
@@ -20,6 +20,9 @@ struct Args {
     float sign;
     KsaDivisor by_parts, by_rows, by_w;
     int32_t w;
+    const int32_t *pos;           // [batch]; one row of each sequence
+    int32_t per_position, most;   // summaries of a chunk (0: text indices); what is from `most` on is outside
+    KsaDivisor by_position;
 };
 
 // Outputs of this many bytes and more, which the caches (256 MB behind the L2s) cannot keep for whoever reads them next, go past them: 36864 rows, 40 heads of 128, 378 MB
@@ -34,10 +37,25 @@ __global__ __launch_bounds__(256) void ksa_rotary_kernel(const Args a) {
     const int unit = (int)blockIdx.x * 4 + wave;
     if (unit >= a.units) return;
     const int row = ksa_div(unit, a.by_parts), part = unit - row * a.parts, b = ksa_div(row, a.by_rows), at = row - b * a.rows;
-    const int j = ksa_div(at, a.by_w), position = j * a.c + min(at - j * a.w, a.c - 1);
     const int piece = lane % LANES;
-    const Turn t = turn_at<P>(a.rotary, position, a.sign, piece, table[wave]);
     const int all = a.heads[0] + a.heads[1], step = PER * a.parts;
+    int position;
+    if (a.pos) {
+        const int p = a.pos[b];
+        if ((unsigned)p >= (unsigned)a.most) {
+            for (int h = part * PER + lane / LANES; h < all; h += step) {
+                const int of = h >= a.heads[0] ? 1 : 0, head = h - (of ? a.heads[0] : 0);
+                __bf16 *const to = of ? a.out[1] + b * a.out_batch[1] + head * a.out_head[1] : a.out[0] + b * a.out_batch[0] + head * a.out_head[0];
+                *reinterpret_cast<u32x4 *>(to + piece * 8) = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};   // NaN
+            }
+            return;
+        }
+        position = a.per_position ? ksa_div(p, a.by_position) * a.c + a.c - 1 : p;   // (a summary's: the last text of its chunk)
+    } else {
+        const int j = ksa_div(at, a.by_w);
+        position = j * a.c + min(at - j * a.w, a.c - 1);
+    }
+    const Turn t = turn_at<P>(a.rotary, position, a.sign, piece, table[wave]);
     for (int h0 = part * PER + lane / LANES; h0 < all; h0 += step * AT_ONCE) {
         Piece<P> x[AT_ONCE];
 #pragma unroll
@@ -83,14 +101,17 @@ int ksa_launch_rotary(const KsaRotaryCall &L, void *stream) {
         a.out_batch[x] = L.out_strides[x][0], a.out_row[x] = L.out_strides[x][1], a.out_head[x] = L.out_strides[x][2];
     }
     a.heads[0] = L.in[0] ? L.p.n_q_heads : 0, a.heads[1] = L.in[1] ? L.p.n_kv_heads : 0;
-    a.rows = L.aug_len;
-    const int rows = L.aug_len * L.p.batch, accesses = ((a.heads[0] + a.heads[1]) * L.p.head_dim + 511) / 512;
+    a.rows = L.rows;
+    const int rows = L.rows * L.p.batch, accesses = ((a.heads[0] + a.heads[1]) * L.p.head_dim + 511) / 512;
     // Few rows: a row's heads are dealt to several waves, up to 4096 of them. Two calls, with 1024, 4096 and 16384 (us): 112 rows 5.9, 6.2, 6.2; 450 rows 8.4, 9.0, 9.3;
     // 1700 rows 18.9, 17.7, 22.5; 3400 rows 28.0, 27.9, 26.6.
     a.parts = std::max(1, std::min(accesses, 4096 / rows));
     a.units = rows * a.parts;
     a.c = L.p.chunk_len, a.w = a.c + (L.p.chunk_len > L.p.n_text ? 0 : L.p.n_summary);   // (a chunk that is never whole has no summaries)
     a.sign = L.back ? -1.f : 1.f;
+    a.pos = L.pos, a.per_position = L.kind == KSA_ROW_SUMMARY ? L.p.n_summary : 0;
+    a.most = L.kind == KSA_ROW_SUMMARY ? L.p.n_text / L.p.chunk_len * L.p.n_summary : L.p.n_text;
+    a.by_position = ksa_divisor(std::max(a.per_position, 1));
     a.by_parts = ksa_divisor(a.parts), a.by_rows = ksa_divisor(a.rows), a.by_w = ksa_divisor(a.w);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (L.p.head_dim == 128) launch<128>(a, rotary_pairs(L.rotary), st);

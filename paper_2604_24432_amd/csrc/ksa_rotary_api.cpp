@@ -14,15 +14,13 @@ bool rotary_strides(int64_t out[3], const int64_t *given, int64_t rows, int32_t 
     return true;
 }
 
-int rotary_call(const ksa_params *p, const ksa_rotary *rotary, const void *q, const void *k, void *q_out, void *k_out, const int64_t *qs, const int64_t *ks,
-                const int64_t *qos, const int64_t *kos, bool back, void *stream) {
-    const int rc = ksa_validate_params(p);
-    if (rc != KSA_OK) return rc;
+// rows: of a sequence
+int rotary_call(const ksa_params *p, const ksa_rotary *rotary, int64_t rows, const void *q, const void *k, void *q_out, void *k_out, const int64_t *qs, const int64_t *ks,
+                const int64_t *qos, const int64_t *kos, bool back, const int32_t *pos, int32_t kind, void *stream) {
     if (ksa_check_rotary(rotary, p->head_dim) != KSA_OK) return KSA_ERR_INVALID_ARG;
     if ((q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr) || (!q && !k)) return KSA_ERR_INVALID_ARG;
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16)) return KSA_ERR_INVALID_ARG;
     KsaRotaryCall a;
-    const int64_t rows = augmented(p);
     const int32_t heads[2] = {p->n_q_heads, p->n_kv_heads};
     const int64_t *const in[2] = {qs, ks}, *const out[2] = {qos, kos};
     a.in[0] = q, a.in[1] = k, a.out[0] = q_out, a.out[1] = k_out;
@@ -31,8 +29,13 @@ int rotary_call(const ksa_params *p, const ksa_rotary *rotary, const void *q, co
             !rotary_strides(a.out_strides[x], a.in[x] ? out[x] : nullptr, rows, heads[x], p->head_dim))
             return KSA_ERR_INVALID_ARG;
     if (rows * p->batch >= ((int64_t)1 << 26)) return KSA_ERR_UNSUPPORTED;   // a wave each, of a grid of 2^32 lanes
-    a.p = *p, a.rotary = *rotary, a.aug_len = (int32_t)rows, a.back = back;
+    a.p = *p, a.rotary = *rotary, a.rows = (int32_t)rows, a.back = back, a.pos = pos, a.kind = kind;
     return ksa_launch_rotary(a, stream);
+}
+int rotary_call(const ksa_params *p, const ksa_rotary *rotary, const void *q, const void *k, void *q_out, void *k_out, const int64_t *qs, const int64_t *ks,
+                const int64_t *qos, const int64_t *kos, bool back, void *stream) {
+    const int rc = ksa_validate_params(p);
+    return rc != KSA_OK ? rc : rotary_call(p, rotary, augmented(p), q, k, q_out, k_out, qs, ks, qos, kos, back, nullptr, KSA_ROW_TEXT, stream);
 }
 
 }  // namespace
@@ -68,6 +71,19 @@ int ksa_rotary_fwd(const ksa_params *p, const ksa_rotary *rotary, const void *q,
 int ksa_rotary_bwd(const ksa_params *p, const ksa_rotary *rotary, const void *dq_out, const void *dk_out, void *dq, void *dk, const int64_t dq_out_strides[3],
                    const int64_t dk_out_strides[3], const int64_t dq_strides[3], const int64_t dk_strides[3], void *stream) {
     return rotary_call(p, rotary, dq_out, dk_out, dq, dk, dq_out_strides, dk_out_strides, dq_strides, dk_strides, true, stream);
+}
+
+int ksa_rotary_step(const ksa_params *p, const ksa_rotary *rotary, int32_t kind, const void *q, const void *k, const int32_t *pos, void *q_out, void *k_out,
+                    const int64_t q_strides[2], const int64_t k_strides[2], const int64_t q_out_strides[2], const int64_t k_out_strides[2], void *stream) {
+    const int rc = ksa_validate_params(p);
+    if (rc != KSA_OK) return rc;
+    if ((kind != KSA_ROW_TEXT && kind != KSA_ROW_SUMMARY) || (kind == KSA_ROW_SUMMARY && p->n_summary == 0) || !pos || !aligned(pos, 4)) return KSA_ERR_INVALID_ARG;
+    const int64_t *const given[4] = {q_strides, k_strides, q_out_strides, k_out_strides};
+    int64_t with_rows[4][3];      // a row's stride is of no account
+    for (int x = 0; x < 4; ++x)
+        if (given[x]) with_rows[x][0] = with_rows[x][1] = given[x][0], with_rows[x][2] = given[x][1];
+    auto strides = [&](int x) { return given[x] ? with_rows[x] : nullptr; };
+    return rotary_call(p, rotary, 1, q, k, q_out, k_out, strides(0), strides(1), strides(2), strides(3), false, pos, kind, stream);
 }
 
 int ksa_paged_rotary(const ksa_params *p, const ksa_paged_cache *cache, const ksa_rotary *rotary, const void *q, void *q_out, const void *k_new, const void *v_new,

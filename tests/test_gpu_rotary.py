@@ -335,3 +335,74 @@ def test_outputs_larger_than_the_caches(rule):
     inout = q.clone()
     K.ksa_rotary_bwd(p, r, inout, None, inout)
     assert torch.equal(bits(inout), bits(got[0]))
+
+
+@pytest.mark.parametrize("rule", [RULES[0], RULES[1], RULES[3], RULES[4], RULES[6]], ids=name)
+@pytest.mark.parametrize("B,Hq,Hkv,d,c,m", [(1, 1, 1, 64, 16, 2), (5, 32, 8, 128, 64, 8), (300, 7, 7, 128, 8, 1), (3, 12, 4, 64, 48, 6)])
+def test_single_rows_of_the_decode_loop(B, Hq, Hkv, d, c, m, rule):
+    """The bits of the whole sequence's rows; sequences whose position is outside become NaN; in place, strided, q or k alone."""
+    rule = {**rule, "dim": min(rule["dim"], d)}
+    say(f"rotary step {B} {Hq}/{Hkv} {d} {rule}")
+    n = 10 * c + c // 2
+    p = K.make_params(B, n, c, m, 1, Hq, Hkv, d)
+    one = K.make_params(1, n, c, m, 1, Hq, Hkv, d)
+    L = K.binding.augmented_rows(p, n)
+    r = handle(rule)
+    q, k = randn(B, Hq, d, seed=1), randn(B, Hkv, d, seed=2)
+    for kind, most in ((K.KSA_ROW_TEXT, n), (K.KSA_ROW_SUMMARY, 10 * m)):
+        at = [(b * 37 + most - 1) % most for b in range(B)]
+        pos = torch.tensor(at, dtype=torch.int32, device="cuda")
+        q_out, k_out = K.ksa_rotary_step(p, r, kind, q, k, pos)
+        rows = [x // c * (c + m) + x % c if kind == K.KSA_ROW_TEXT else x // m * (c + m) + c + x % m for x in at]
+        within(q_out, q, rule, positions(rows, c, m)), within(k_out, k, rule, positions(rows, c, m))
+        b = B // 2
+        line = torch.zeros(1, L, Hq, d, dtype=torch.bfloat16, device="cuda")
+        line[0, rows[b]] = q[b]
+        assert torch.equal(bits(K.ksa_rotary_fwd(one, r, line, None)[0][0, rows[b]]), bits(q_out[b]))
+        only_q, none = K.ksa_rotary_step(p, r, kind, q, None, pos)
+        none_, only_k = K.ksa_rotary_step(p, r, kind, None, k, pos)
+        assert none is None and none_ is None and torch.equal(bits(only_q), bits(q_out)) and torch.equal(bits(only_k), bits(k_out))
+        fused = torch.cat([q, k], 1)
+        K.ksa_rotary_step(p, r, kind, fused[:, :Hq], fused[:, Hq:], pos, fused[:, :Hq], fused[:, Hq:])
+        assert torch.equal(bits(fused), bits(torch.cat([q_out, k_out], 1)))
+        for outside in (-1, most, 2 ** 31 - 1):
+            bad = pos.clone()
+            bad[b] = outside
+            got_q, got_k = K.ksa_rotary_step(p, r, kind, q, k, bad)
+            others = torch.arange(B, device="cuda") != b
+            assert bool(torch.isnan(got_q[b]).all()) and bool(torch.isnan(got_k[b]).all())
+            assert torch.equal(bits(got_q[others]), bits(q_out[others])) and torch.equal(bits(got_k[others]), bits(k_out[others]))
+
+
+def test_a_decode_loop_with_positions_agrees_with_the_prefill():
+    """Keys turned before they are cached, queries before they attend: a generate loop's rows are those of the whole sequence turned and prefilled."""
+    say("rotary decode loop")
+    c, m, n = 16, 2, 80
+    p = K.make_params(2, n, c, m, 1, 4, 2, 64)
+    lay = K.Layout(p)
+    L = lay.aug_len
+    r = handle(dict(dim=64, base=1000.0))
+    q, k, v = randn(2, L, 4, 64, seed=1), randn(2, L, 2, 64, seed=2), randn(2, L, 2, 64, seed=3)
+    want, _ = K.ksa_prefill_fwd(lay, *K.ksa_rotary_fwd(p, r, q, k), v)
+    _, rows = K.cache_geometry(p)
+    kc, vc = (torch.zeros(2, 2, rows, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for a in range(L):
+        j, x = divmod(a, c + m)
+        kind, at = (K.KSA_ROW_TEXT, j * c + x) if x < c else (K.KSA_ROW_SUMMARY, j * m + x - c)
+        pos = torch.full((2,), at, dtype=torch.int32, device="cuda")
+        q1, k1 = K.ksa_rotary_step(p, r, kind, q[:, a], k[:, a], pos)
+        K.ksa_cache_append(p, kind, k1.contiguous(), v[:, a].contiguous(), pos, kc, vc)
+        o, _ = (K.ksa_decode_fwd if kind == K.KSA_ROW_TEXT else K.ksa_decode_summary_fwd)(p, q1.contiguous(), kc, vc, pos)
+        # two kernels' bars against the definition, 2e-2 each
+        assert float((o.float() - want[:, a].float()).abs().max()) <= 4e-2, a
+
+
+def test_python_refuses_single_rows_that_do_not_fit():
+    p = K.make_params(2, 100, 16, 2, 1, 4, 2, 128)
+    r = handle(RULES[0])
+    q, k, pos = randn(2, 4, 128), randn(2, 2, 128), torch.zeros(2, dtype=torch.int32, device="cuda")
+    for bad in ((q[:1], k, pos), (q, q, pos), (q.float(), k, pos), (None, None, pos), (q, k, pos[:1]), (q, k, pos.long()), (q, k, pos.cpu()), (q.cpu(), k, pos), (None, k, pos, q)):
+        with pytest.raises(ValueError):
+            K.ksa_rotary_step(p, r, K.KSA_ROW_TEXT, *bad)
+    with pytest.raises(K.KsaError):
+        K.ksa_rotary_step(p, r, 5, q, k, pos)

@@ -85,3 +85,18 @@ def test_new_rows_are_refused():
     assert paged(p=params(head_dim=32)) == UNSUPPORTED
     assert paged(p=params(n_q_heads=1, n_kv_heads=1), total=2 ** 26) == UNSUPPORTED
     assert paged(total=0, q=None, q_out=None, k=None, v=None) == 0
+
+
+def step(p=None, r=None, kind=0, q=PTR, k=PTR, pos=PTR, q_out=PTR, k_out=PTR, qs=None, ks=None, qos=None, kos=None):
+    i64 = lambda x: (C.c_int64 * 2)(*x) if x else None  # noqa: E731
+    r = rotary() if r is None else r
+    return binding.lib().ksa_rotary_step(C.byref(params() if p is None else p), C.byref(r) if r else None, kind, q, k, pos, q_out, k_out, i64(qs), i64(ks), i64(qos), i64(kos), None)
+
+
+def test_single_rows_are_refused():
+    for bad in BAD:
+        assert step(r=rotary(**bad)) == INVALID, bad
+    for bad in (dict(r=False), dict(kind=2), dict(kind=-1), dict(kind=1, p=params(n_summary=0)), dict(pos=None), dict(pos=PTR + 2), dict(q=None), dict(q_out=None), dict(k=None), dict(k_out=None),
+                dict(q=None, k=None, q_out=None, k_out=None), dict(q=PTR + 8), dict(k_out=PTR + 2), dict(qs=(0, 128)), dict(ks=(256, 12)), dict(qos=(1024, -128)), dict(kos=(4, 128))):
+        assert step(**bad) == INVALID, bad
+    assert step(p=params(batch=0)) == INVALID and step(p=params(head_dim=96)) == UNSUPPORTED
