@@ -415,3 +415,49 @@ def test_a_stream_of_its_own():
     assert torch.equal(kb.double(), e2m1(k.double())[0])
     o1, lse1 = K.ksa_paged_fwd(pages.cache, q, *batch_of([899, 899], [1, 1]), max_rows=1)
     assert torch.equal(bits(o), bits(o1)) and torch.equal(lse, lse1)
+
+
+@pytest.mark.parametrize("rows,n_splits", [(1, 1), (1, 3), (6, 1), (60, 1), (60, 2)])
+def test_outputs_in_the_queries_place_and_strided(rows, n_splits):
+    say(f"fp4 in place rows={rows} splits={n_splits}")
+    p = K.make_params(3, 2048, 16, 2, 3, 8, 2, 128)
+    pages = Pages4(p, [900] * 3, 16, 3)
+    for b in range(3):
+        pages.put(b, 0, randn(900, 2, 128, seed=b), randn(900, 2, 128, seed=b + 9))
+    q = randn(3 * rows, 8, 128, seed=5)
+    cu, start = batch_of([500, 899 - rows, 0], [rows] * 3)
+    o, lse = K.ksa_paged_fwd(pages.cache, q, cu, start, max_rows=rows, n_splits=n_splits)
+    x = q.clone()
+    K.ksa_paged_fwd(pages.cache, x, cu, start, max_rows=rows, n_splits=n_splits, o=x, return_lse=False)
+    assert torch.equal(bits(x), bits(o))
+    wide = torch.full((3 * rows, 3, 10, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    wide[:, 0, :8] = q
+    K.ksa_paged_fwd(pages.cache, wide[:, 0, :8], cu, start, max_rows=rows, n_splits=n_splits, o=wide[:, 2, 1:9], return_lse=False)
+    assert torch.equal(bits(wide[:, 2, 1:9]), bits(o)) and torch.equal(bits(wide[:, 0, :8]), bits(q))
+    assert bool((wide[:, 1] == 7).all()) and bool((wide[:, 2, 0] == 7).all()) and bool((wide[:, 2, 9] == 7).all())
+
+
+@pytest.mark.parametrize("rows", [1, 60])
+def test_products_that_overflow_before_they_are_scaled(rows):
+    """q k beyond 3.4e38 whose scaled scores are not: the power of two of the scale that goes into q keeps them finite."""
+    say(f"fp4 large products {rows}")
+    d = 128
+    p = K.make_params(1, 1024, 16, 2, 3, 4, 2, d, softmax_scale=2.0 ** -8)
+    pages = Pages4(p, [300], 16, 3)
+    k, v = randn(300, 2, d, seed=1), randn(300, 2, d, seed=2)
+    big = torch.zeros_like(k)
+    big[..., 0] = k[..., 0].sign() * 2.0 ** 63                          # one element each: q k = +- 2^132 before, +- 2^124 after the scale
+    big[150:, :, 0] = 0.0
+    pages.put(0, 0, big, v)
+    q = torch.zeros(rows, 4, d, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 2.0 ** 69
+    first = 300 - rows
+    o, lse = K.ksa_paged_fwd(pages.cache, q, *batch_of([first], [rows]), max_rows=rows)
+    kk, vv = e2m1(big.double())[0], e2m1(v.double())[0]
+    see = torch.from_numpy(mask(np.arange(first, 300), 300, 16, 2, 3)).cuda()
+    for h in range(4):
+        s = (q[:, h].double() @ kk[:, h // 2].T * 2.0 ** -8).masked_fill(~see, -math.inf)
+        want = torch.softmax(s, 1) @ vv[:, h // 2]
+        assert bool(torch.isfinite(o[:, h].float()).all()) and bool(torch.isfinite(lse[:, h]).all())
+        # equal scores have equal weights: the mean of some values, to the roundings of bf16 (weights of 1, the output) and of 300 sums
+        assert bool(((o[:, h].double() - want).abs() <= 2.0 ** -8 * want.abs() + 300 * 2.0 ** -24 * float(vv.abs().max())).all()), h

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from tests.paged_fp4 import LEVELS, e2m1
-from tests.test_paged_host import INVALID, PTR, TOO_SMALL, cache, fwd, move
+from tests.test_paged_host import INVALID, PTR, TOO_SMALL, UNSUPPORTED, cache, fwd, move
 
 
 def cache4(**more):
@@ -37,3 +37,12 @@ def test_the_definition_rounds_to_the_nearest_and_loses_no_more_than_half_a_step
     assert bool((LEVELS[(code % 8).long()] * scale == value.abs()).all())
     halfway = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0] + [0.0] * 24, dtype=torch.float64)
     assert e2m1(halfway)[0][:8].tolist() == [0.0, 1.0, 1.0, 2.0, 2.0, 4.0, 4.0, 6.0]
+
+
+def test_pages_too_far_apart_are_refused():
+    """Places within a page, and from page to page, are 32 bits."""
+    for strides in ((2 ** 32, 2048, 64), (2 ** 40, 2048, 64), (2 ** 33, 2048, 2 ** 28), (4096, 2048, 2 ** 28)):
+        c = cache4(strides=(C.c_int64 * 3)(*strides))
+        assert move("ksa_paged_append", c=c) == UNSUPPORTED and move("ksa_paged_read", c=c) == UNSUPPORTED and fwd(c=c) == UNSUPPORTED, strides
+    for strides in ((2 ** 32 - 16, 2048, 64), (2 ** 32 - 16, 2 ** 40, 64), (4096, 2048, 2 ** 28 - 16)):      # (16 rows; heads may lie anywhere)
+        assert fwd(c=cache4(strides=(C.c_int64 * 3)(*strides))) == TOO_SMALL, strides
