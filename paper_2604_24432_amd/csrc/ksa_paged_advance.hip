@@ -260,8 +260,8 @@ __global__ __launch_bounds__(N) void ksa_advance_take_kernel(const Args a) {
         __syncthreads();
     }
     if (!a.rows_here) return;
-    const int held = a.held[b];
-    for (int x = threadIdx.x; x < s.rows && rows_before + x < a.rows.total; x += N) describe(a, rows_before + x, s.start + x, b, text_before, held);
+    const int held = a.held[b], mapped = min(s.rows, a.rows.total - rows_before);   // (a row's place may be beyond 32 bits where it is beyond the maps)
+    for (int x = threadIdx.x; x < mapped; x += N) describe(a, rows_before + x, s.start + x, b, text_before, held);
     for (int64_t row = (int64_t)all_rows + b * N + threadIdx.x; row < a.rows.total; row += (int64_t)batch * N) describe_none(a, (int)row);
 }
 

@@ -305,3 +305,28 @@ def test_two_graphs_share_a_workspace():
         torch.cuda.synchronize()
         for (books, total, held, new, step, graph, lengths), want in zip(made, wants):
             books.check(step, want, total)
+
+
+@pytest.mark.parametrize("batch", [3, 5, 4099])
+def test_more_rows_than_32_bits_in_a_step_whose_maps_are_short(batch):
+    say(f"advance rows beyond 32 bits, {batch}")
+    n, c, m, page, total, some = 2 ** 29, 16, 4, 8, 40, 6
+    p = K.make_params(batch, n, c, m, 2, 1, 1, 64)
+    L = n + n // c * m                                                      # of a sequence: 3 and more of them pass 2^31 - 256
+    pool = torch.zeros(40, 1, page, 64, dtype=torch.bfloat16, device="cuda")
+    text, sums = (torch.full((batch, cols), -1, dtype=torch.int32, device="cuda") for cols in (4, 2))
+    refs = torch.zeros(40, dtype=torch.int32, device="cuda")
+    cache = K.PagedCache(p, pool, pool, text, sums)
+    held, new = (torch.full((batch,), x, dtype=torch.int32, device="cuda") for x in (0, n))
+    step = K.ksa_paged_advance(cache, refs, held, new, total)
+    assert step.cu_rows.tolist() == [min(b * L, 2 ** 31 - 1) for b in range(batch + 1)] and step.start.tolist() == [0] * batch
+    assert step.lacking.tolist() == [max(batch * 6 - 40, 0)]
+    got = torch.cat([text, sums], 1)[:some].tolist()
+    assert got == [[6 * b + x if 6 * b + x < 40 else -1 for x in range(6)] for b in range(min(batch, some))]
+    want = []
+    for row in range(total):                                                # all of the first sequence
+        j, r = divmod(row, c + m)
+        idx = j * c + r if r < c else j * m + r - c
+        col, at = idx // page, idx % page
+        want.append((((col if r < c else 4 + col) * page + at) if col < (4 if r < c else 2) else -1, j * c + min(r, c - 1), idx if r < c else c - 1 - r))
+    assert list(zip(step.slots.tolist(), step.positions.tolist(), step.tokens.tolist())) == want
