@@ -497,8 +497,8 @@ int ksa_paged_rotary(const ksa_params *params /*host*/, const ksa_paged_cache *c
  *   workspace: device, 16-byte aligned, at least ksa_paged_advance_workspace_bytes bytes, needed until the work enqueued on `stream` has finished;
  *   calls that share one must be stream-ordered.
  * Counts beyond 2^31 - 1 (cu_rows) stay there.  Nothing is allocated, cleared or waited for; the call may be captured into a graph.  Results do not depend on the
- * order of execution.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^31 columns of
- * both tables over all sequences, or rows, and more), HIP.
+ * order of execution.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^31 - 4096 columns
+ * of both tables over all sequences and more; total_rows of 2^31 - 256 and more), HIP.
  */
 size_t ksa_paged_advance_workspace_bytes(const ksa_params *params /*host*/, const ksa_paged_cache *cache /*host*/);
 int ksa_paged_advance(const ksa_params *params /*host*/, const ksa_paged_cache *cache /*host*/, int32_t *page_refs, const int32_t *held, const int32_t *new_text,

@@ -3,9 +3,10 @@
 
 namespace {
 
-// Pages and columns for which every index and count of pages fits 32 bits.
+// Columns for which every index and count of them fits 32 bits, a workgroup's step behind the last one among them.
+constexpr int64_t MOST_COLUMNS = ((int64_t)1 << 31) - 4096;
 bool too_large(const ksa_params *p, const ksa_paged_cache *cache) {
-    return p->batch * ((int64_t)cache->text_pages + cache->summary_pages) >= (int64_t)1 << 31;
+    return p->batch * ((int64_t)cache->text_pages + cache->summary_pages) >= MOST_COLUMNS;
 }
 
 size_t bytes_of(const ksa_params *p, const ksa_paged_cache *cache) { return (ksa_paged_advance_ints(p->batch, cache->n_pages) * sizeof(int32_t) + 15) / 16 * 16; }

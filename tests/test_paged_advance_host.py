@@ -71,3 +71,12 @@ def test_the_model_keeps_its_books(seed):
         for b in range(B):
             lost[b] = new[b] >= 0 and (lost[b] or any(r[0] < 0 for r in rows[cu[b]:cu[b + 1]]))
             held[b] = 0 if new[b] < 0 else held[b] + new[b]
+
+
+def test_columns_and_rows_whose_steps_pass_32_bits_are_refused():
+    """A workgroup goes over columns 2048 at a time: a step behind the last one has to fit 32 bits too."""
+    p, c = params(batch=1), lambda n: cache(text_pages=n, summary_pages=8)
+    for n in (2 ** 31 - 4096 - 8, 2 ** 31 - 2048, 2 ** 31 - 9, 2 ** 31 - 1):
+        assert call(p=p, c=c(n)) == UNSUPPORTED and need(p, c(n)) == 0, n
+    assert need(p, c(2 ** 31 - 4096 - 9)) > 0 and call(p=p, c=c(2 ** 31 - 4096 - 9), ws_bytes=0) == TOO_SMALL
+    assert call(total=2 ** 31 - 256) == UNSUPPORTED and call(total=2 ** 31 - 257, ws_bytes=0) == TOO_SMALL
