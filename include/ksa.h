@@ -449,7 +449,7 @@ int ksa_rotary_turns(const ksa_rotary_rule *rule /*host*/, uint64_t *turns /*hos
  * device bf16, last dim contiguous.  q and q_out, or k and k_out, may be NULL.  An output may be the memory of its input (same strides).
  * *_strides = {batch, row, head} in elements, multiples of 8, positive; NULL = contiguous.  Angles and products are fp32, each output is rounded once.
  * ksa_rotary_bwd: gradients with respect to q and k from those with respect to what ksa_rotary_fwd gave: turned back, times magnitude.
- * Errors: INVALID_ARG (null or misaligned pointers: 16 bytes; bad strides or rotary fields), UNSUPPORTED (2^26 rows of all sequences and more), HIP.
+ * Errors: INVALID_ARG (null or misaligned pointers: 16 bytes; bad strides or rotary fields), UNSUPPORTED (more than 2^26 - 4 rows of all sequences), HIP.
  */
 int ksa_rotary_fwd(const ksa_params *params /*host*/, const ksa_rotary *rotary /*host*/, const void *q, const void *k, void *q_out, void *k_out,
                    const int64_t q_strides[3], const int64_t k_strides[3], const int64_t q_out_strides[3], const int64_t k_out_strides[3], void *stream);
@@ -467,7 +467,7 @@ int ksa_rotary_step(const ksa_params *params /*host*/, const ksa_rotary *rotary 
 /*
  * ksa_paged_rotary: a serving step's new rows in one launch: q (device bf16 [total_rows, Hq, d]) is turned into q_out, k_new is turned, and goes with v_new into the
  * cache, as ksa_paged_append puts it (k is rounded to bf16 in between: the same bits as in two steps).  Batch, tables, capacity and errors as there (and UNSUPPORTED
- * from 2^26 rows on); rows of q of a sequence out of place become NaN in q_out.  q and q_out may be NULL; q_out may be the memory of q (same strides).
+ * above 2^26 - 4 rows); rows of q of a sequence out of place become NaN in q_out.  q and q_out may be NULL; q_out may be the memory of q (same strides).
  */
 int ksa_paged_rotary(const ksa_params *params /*host*/, const ksa_paged_cache *cache /*host*/, const ksa_rotary *rotary /*host*/, const void *q, void *q_out,
                      const void *k_new, const void *v_new, const int64_t q_strides[2], const int64_t q_out_strides[2], const int64_t kv_strides[2],

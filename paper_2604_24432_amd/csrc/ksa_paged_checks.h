@@ -73,6 +73,8 @@ inline int check_strides(int64_t out[2], const int64_t *given, int32_t heads, in
 }
 
 constexpr int64_t MOST_LANES = (int64_t)1 << 32;   // of a grid, none of its dimensions more
+// A launch with a wave per row, four to a workgroup: 2^26 - 4 rows are the most.
+inline bool too_many_waves(int64_t rows) { return (rows + 3) / 4 * 256 >= MOST_LANES; }
 
 inline int move_call(KsaPagedMove &a, const ksa_params *p, const ksa_paged_cache *cache, const void *k, const void *v, const int64_t *strides,
               const int32_t *cu_rows, const int32_t *start, int64_t total_rows) {

@@ -28,7 +28,7 @@ int rotary_call(const ksa_params *p, const ksa_rotary *rotary, int64_t rows, con
         if (!rotary_strides(a.in_strides[x], a.in[x] ? in[x] : nullptr, rows, heads[x], p->head_dim) ||
             !rotary_strides(a.out_strides[x], a.in[x] ? out[x] : nullptr, rows, heads[x], p->head_dim))
             return KSA_ERR_INVALID_ARG;
-    if (rows * p->batch >= ((int64_t)1 << 26)) return KSA_ERR_UNSUPPORTED;   // a wave each, of a grid of 2^32 lanes
+    if (too_many_waves(rows * p->batch)) return KSA_ERR_UNSUPPORTED;
     a.p = *p, a.rotary = *rotary, a.rows = (int32_t)rows, a.back = back, a.pos = pos, a.kind = kind;
     return ksa_launch_rotary(a, stream);
 }
@@ -96,7 +96,7 @@ int ksa_paged_rotary(const ksa_params *p, const ksa_paged_cache *cache, const ks
     if ((q != nullptr) != (q_out != nullptr) || !aligned(q, 16) || !aligned(q_out, 16)) return KSA_ERR_INVALID_ARG;
     if ((rc = check_strides(a.q_strides, q ? q_strides : nullptr, p->n_q_heads, p->head_dim)) != KSA_OK) return rc;
     if ((rc = check_strides(a.out_strides, q ? q_out_strides : nullptr, p->n_q_heads, p->head_dim)) != KSA_OK) return rc;
-    if (total_rows >= (int64_t)1 << 26) return KSA_ERR_UNSUPPORTED;   // a wave each, of a grid of 2^32 lanes
+    if (too_many_waves(total_rows)) return KSA_ERR_UNSUPPORTED;
     if (total_rows == 0) return KSA_OK;
     a.move.k = const_cast<void *>(k_new), a.move.v = const_cast<void *>(v_new);   // (read only)
     a.rotary = *rotary, a.q = q, a.q_out = q_out;

@@ -100,3 +100,14 @@ def test_single_rows_are_refused():
                 dict(q=None, k=None, q_out=None, k_out=None), dict(q=PTR + 8), dict(k_out=PTR + 2), dict(qs=(0, 128)), dict(ks=(256, 12)), dict(qos=(1024, -128)), dict(kos=(4, 128))):
         assert step(**bad) == INVALID, bad
     assert step(p=params(batch=0)) == INVALID and step(p=params(head_dim=96)) == UNSUPPORTED
+
+
+def test_rows_whose_launch_would_have_2_to_the_32_lanes_are_refused():
+    """A row takes a wave, four of them a workgroup of 256, and a launch has less than 2^32 lanes: 2^26 - 4 rows are the most."""
+    for rows in (2 ** 26 - 3, 2 ** 26 - 2, 2 ** 26 - 1, 2 ** 26):
+        p = params(batch=1, n_text=rows, chunk_len=64, n_summary=0)
+        for entry in ("ksa_rotary_fwd", "ksa_rotary_bwd"):
+            assert whole(entry, p=p) == UNSUPPORTED, (entry, rows)
+        assert paged(p=params(n_q_heads=1, n_kv_heads=1), total=rows) == UNSUPPORTED, rows
+    for entry in ("ksa_rotary_fwd", "ksa_rotary_bwd"):
+        assert whole(entry, p=params(batch=3, n_text=(2 ** 26 - 1) // 3, chunk_len=64, n_summary=0)) == UNSUPPORTED
