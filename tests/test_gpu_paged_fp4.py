@@ -461,3 +461,50 @@ def test_products_that_overflow_before_they_are_scaled(rows):
         assert bool(torch.isfinite(o[:, h].float()).all()) and bool(torch.isfinite(lse[:, h]).all())
         # equal scores have equal weights: the mean of some values, to the roundings of bf16 (weights of 1, the output) and of 300 sums
         assert bool(((o[:, h].double() - want).abs() <= 2.0 ** -8 * want.abs() + 300 * 2.0 ** -24 * float(vv.abs().max())).all()), h
+
+
+# pages, of which the last ones are used, every gap-th; bytes from page to page
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_pages,gap,stride", [(8, 1, 1 << 30), ((1 << 25) + 200, 16, 272)], ids=["1 GiB apart", "exponents beyond 4 GiB"])
+def test_rows_and_exponents_beyond_32_bits(n_pages, gap, stride, d):
+    """Pools and exponents larger than 4 GiB: every byte where it belongs, by append and by the rotary call, and found there by all that reads.  (The pages lie
+    closer to each other than they are long, where only every 16th is used.)"""
+    say(f"fp4 beyond 32 bits {n_pages} {stride} d={d}")
+    page, n, c, m = 64, 300, 64, 8
+    p = K.make_params(1, 512, c, m, 1, 2, 1, d)
+    cols = K.paged_pages(p, page, n)
+    used = [n_pages - 1 - gap * x for x in range(sum(cols))]
+    assert min(used) >= 0 and max(used) * stride >= 2 ** 32 and (gap == 1 or min(used) * page * (d // 32) >= 2 ** 32) and gap * stride >= page * d // 2
+    text, sums = (torch.tensor([x], dtype=torch.int32, device="cuda") for x in (used[:cols[0]], used[cols[0]:]))
+
+    def pool():
+        far = torch.empty((n_pages - 1) * stride + page * d // 2, dtype=torch.uint8, device="cuda")
+        return torch.as_strided(far, (n_pages, 1, page, d // 2), (stride, page * d // 2, d // 2, 1))
+
+    pools, exps = [pool(), pool()], [torch.zeros(n_pages, 1, page, d // 32, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    cache = K.PagedCache(p, *pools, text, sums, *exps)
+    _, is_text, idx = kinds(n, c, m)
+    at = torch.tensor([(used[:cols[0]] if t else used[cols[0]:])[i // page] for t, i in zip(is_text, idx)], device="cuda")
+    slot = torch.from_numpy(idx % page).cuda()
+    cu, start = batch_of([0], [n])
+    k, v = randn(n, 1, d, seed=1), randn(n, 1, d, seed=2)
+
+    def holds(*rows):
+        for x, pool_of, exp_of in zip(rows, pools, exps):
+            _, code, e = e2m1(x.double())
+            assert torch.equal(pool_of[at, :, slot], packed(code)) and torch.equal(exp_of[at, :, slot], e)
+
+    rotary, line = K.Rotary(d), torch.zeros(1, K.binding.augmented_rows(p, 512), 1, d, dtype=torch.bfloat16, device="cuda")
+    line[0, :n] = k
+    K.ksa_paged_rotary(cache, rotary, None, k, v, cu, start)
+    holds(K.ksa_rotary_fwd(p, rotary, None, line)[1][0, :n], v)
+    K.ksa_paged_append(cache, k, v, cu, start)
+    holds(k, v)
+    value = [e2m1(x.double())[0] for x in (k, v)]
+    for got, want in zip(K.ksa_paged_read(cache, cu, start, n), value):
+        assert torch.equal(got.double(), want)
+    for rows in (1, 10, 100):                                             # 2 and 20 pairs of rows and heads, then tiles of them
+        q = randn(rows, 2, d, seed=3)
+        o, lse = K.ksa_paged_fwd(cache, q, *batch_of([n - rows], [rows]), max_rows=rows)
+        want, want_lse, off, lse_off = bounds(q.double(), *value, list(range(n - rows, n)), p)
+        assert bool(((o.double() - want).abs() <= off).all()) and bool(((lse.double() - want_lse).abs() <= lse_off).all()), rows
