@@ -330,3 +330,29 @@ def test_more_rows_than_32_bits_in_a_step_whose_maps_are_short(batch):
         col, at = idx // page, idx % page
         want.append((((col if r < c else 4 + col) * page + at) if col < (4 if r < c else 2) else -1, j * c + min(r, c - 1), idx if r < c else c - 1 - r))
     assert list(zip(step.slots.tolist(), step.positions.tolist(), step.tokens.tolist())) == want
+
+
+@pytest.mark.parametrize("last", [16 * 6710886 + 7, 16 * 6710886 + 8, 2 ** 29])
+def test_the_last_sequence_alone_is_beyond_32_bits(last):
+    """Three sequences' rows fit 32 bits; with the fourth's there are 2^31 - 1, one more, or many more."""
+    say(f"advance last sequence beyond 32 bits, {last}")
+    n, c, m, page, total, batch = 2 ** 29, 16, 4, 8, 24, 4
+    p = K.make_params(batch, n, c, m, 2, 1, 1, 64)
+    L, last_rows = n + n // c * m, last + last // c * m
+    assert 3 * L < 2 ** 31 - 256 and 3 * L + last_rows - (2 ** 31 - 1) in (0, 1, 4 * L - (2 ** 31 - 1))
+    pool = torch.zeros(40, 1, page, 64, dtype=torch.bfloat16, device="cuda")
+    text, sums = (torch.full((batch, cols), -1, dtype=torch.int32, device="cuda") for cols in (4, 2))
+    refs = torch.zeros(40, dtype=torch.int32, device="cuda")
+    cache = K.PagedCache(p, pool, pool, text, sums)
+    held, new = torch.zeros(batch, dtype=torch.int32, device="cuda"), torch.tensor([n, n, n, last], dtype=torch.int32, device="cuda")
+    step = K.ksa_paged_advance(cache, refs, held, new, total)
+    assert step.cu_rows.tolist() == [0, L, 2 * L, 3 * L, min(3 * L + last_rows, 2 ** 31 - 1)] and step.start.tolist() == [0] * batch
+    assert step.lacking.tolist() == [0] and refs.tolist() == [1] * 24 + [0] * 16
+    assert torch.cat([text, sums], 1).tolist() == [[6 * b + x for x in range(6)] for b in range(batch)]
+    want = []
+    for row in range(total):                                                # all of the first sequence
+        j, r = divmod(row, c + m)
+        idx = j * c + r if r < c else j * m + r - c
+        col, at = idx // page, idx % page
+        want.append((((col if r < c else 4 + col) * page + at) if col < (4 if r < c else 2) else -1, j * c + min(r, c - 1), idx if r < c else c - 1 - r))
+    assert list(zip(step.slots.tolist(), step.positions.tolist(), step.tokens.tolist())) == want
