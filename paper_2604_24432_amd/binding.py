@@ -557,7 +557,7 @@ class PagedCache:
     """A batch of sequences whose K / V rows lie in the pages of one pool (struct ksa_paged_cache); holds its tensors.
 
     k, v: [n_pages, Hkv, page_rows, d] on the GPU, bfloat16, or float8_e4m3fn with k_exp, v_exp uint8 [n_pages, Hkv, page_rows], or 4-bit floats, two to a
-    byte: uint8 [n_pages, Hkv, page_rows, d / 2] with k_exp, v_exp uint8 [n_pages, Hkv, page_rows, d / 32].
+    byte: uint8 [n_pages, Hkv, page_rows, d / 2] with k_exp, v_exp uint8 [n_pages, Hkv, page_rows, d / 32], each at a multiple of 4 bytes.
     text_table, summary_table: int32 [batch, columns], contiguous; their contents may change from call to call.  Other tensors, or other
     parameters, take another PagedCache.  A cache carries no gradient: what is appended, read or attended to is not recorded for autograd.
     """

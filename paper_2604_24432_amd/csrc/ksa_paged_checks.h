@@ -37,7 +37,7 @@ inline int check_cache(KsaPagedCall &c, const ksa_params *p, const ksa_paged_cac
     if (cache->summary_pages < 0 || !aligned(cache->summary_table, 4)) return KSA_ERR_INVALID_ARG;
     if (!cache->k || !cache->v || !aligned(cache->k, 16) || !aligned(cache->v, 16)) return KSA_ERR_INVALID_ARG;
     if (exps != (cache->k_exp != nullptr) || exps != (cache->v_exp != nullptr)) return KSA_ERR_INVALID_ARG;
-    if (f4 && (!aligned(cache->k_exp, 4) || !aligned(cache->v_exp, 4))) return KSA_ERR_INVALID_ARG;   // (a row's bytes are loaded together)
+    if (f4 && (!aligned(cache->k_exp, 4) || !aligned(cache->v_exp, 4))) return KSA_ERR_INVALID_ARG;   // (so that a row's bytes may be loaded together; no kernel does yet)
     const int64_t *s = cache->strides, size = exps ? 1 : 2;   // (of two elements in the 4-bit format)
     if (s[0] == 0 && s[1] == 0 && s[2] == 0) {
         c.cache_strides[2] = f4 ? p->head_dim / 2 : p->head_dim * size;

@@ -118,7 +118,7 @@ __device__ __forceinline__ u32x4 turned(const RotaryArgs &a, const Piece<P> &x, 
         const __bf16 z[2] = {(__bf16)fmaf(lo, t.c[2 * e], lo_of * t.s[2 * e]), (__bf16)fmaf(hi, t.c[2 * e + 1], hi_of * t.s[2 * e + 1])};
         const unsigned z0 = __builtin_bit_cast(unsigned short, z[0]), z1 = __builtin_bit_cast(unsigned short, z[1]);
         const int i = piece * 8 + 2 * e;
-        // (what is not turned keeps its bits; only KSA_HALF_ANY has pieces of both)
+        // (what is not turned keeps its bits; KSA_HALF_ANY, and KSA_NEXT where dim is no multiple of 8, have pieces of both)
         y[e] = (i < a.dim ? z0 : x.own[e] & 0xffffu) | (i + 1 < a.dim ? z1 << 16 : x.own[e] & 0xffff0000u);
     }
     return y;
