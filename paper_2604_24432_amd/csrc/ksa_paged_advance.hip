@@ -33,7 +33,10 @@ constexpr int N = 256, PAGES = 1024;
 // Up to here every workgroup adds up all sequences' counts itself, above one workgroup does it for all, beside those that look for free pages. Each itself and one for all (us):
 // 300 sequences 14.4 and 16.1, 2000 23.0 and 30.2, 4000 40 and 54, 16000 214 and 187.
 constexpr int SUMS_EACH = 4096;
-// Up to so many rows the sequences' own workgroups describe them (all of one sequence: 32 passes), above a launch more does.
+// Up to so many rows the sequences' own workgroups describe them, above a launch more does.  The host knows how long the maps are, and not how many of their rows are one
+// sequence's, which takes 256 of them at a time.  Own workgroups and a launch more (us): 64 rows of 64 sequences 10.7 and 13.3, 7720 of 256 12.1 and 16.0; 56 single rows beside eight
+// times 250 12.4 and 15.3, 500 13.1 and 15.4, 1000 14.3 and 16.1; but 63 beside one of 1000 13.2 and 14.9, 2000 14.8 and 15.1, 4000 17.8 and 15.0, 7500 23.2 and 14.8, so that
+// from 2000 rows of one sequence on the line is too high by up to 8 us.
 constexpr int ROWS_EACH = 8192;
 
 // What a sequence does in a step (columns: of text, of summaries).

@@ -34,6 +34,26 @@ int64_t most_keys(const ksa_params *p, int64_t rows) {
  *                    512  16500                   1: 636    2: 641    4: 656
  *                     16  65536, 8 rows           8: 99    16: 89    32: 91
  * Spans dealt by the sequences' lengths (lengths 1 : 4) instead of the same number each: 57.4 and 53.8 with 128, 248 and 249 with 512.
+ * 4-bit rows, whose kernels are others, are dealt the same way (head_dim 128, four query heads to a KV head, eight where there is one; what is chosen in brackets):
+ *                      1    400                 [1: 6.6]   4: 6.9
+ *                      1    700                  1: 7.9   [5: 8.1]   8: 7.2
+ *                      1   1200                  4: 7.9    8: 7.7   [9: 8.3]
+ *                      1   9000                 16: 10.3  32: 9.7  [64: 9.4]
+ *                      8   6000                  8: 11.3  32: 9.6  [46: 11.1]
+ *                     32    800                  4: 8.4   [6: 8.3]   8: 8.0
+ *                     32   4200                  4: 12.6   8: 10.6 [16: 11.7]  32: 12.4
+ *                     64   1500                  4: 9.2   [5: 10.9]  8: 10.6
+ *                    128   4200                  1: 24.9   2: 19.1  [4: 19.1]   8: 20.0
+ *                    160    800                 [1: 8.3]   2: 11.7
+ *                    256   1500                  1: 13.2  [2: 15.7]
+ *                    256   4000                  1: 27.1  [2: 28.9]  4: 29.3
+ *                    512  16500                 [1: 186]   2: 188    4: 190
+ *                      8   6000, 8 rows          8: 13.8  24: 11.7 [46: 15.3]
+ *                     16  65536, 8 rows          8: 65    16: 41.0 [32: 41.2]  64: 47.5
+ *                     32   4200, 8 rows          4: 16.5   8: 14.3 [16: 18.7]
+ *                    128   9000, 8 rows          2: 44.5  [4: 43.6]  8: 51.0
+ *                    256   1500, 8 rows          1: 17.9  [2: 25.4]  4: 30.9
+ * The best or within 10 % of it in eleven of these, 12 to 42 % above it in the others: spans of few blocks per wave, joins that cost what spans save.
  *
  * Many rows: tiles of 128 pairs, two on a compute unit; of 128, alone, whose two groups of waves have half of the keys each; of 256, alone, which take
  * their keys from memory half as often.  The kind and the spans are chosen by what they are expected to take: a start and an end, the key tiles of
@@ -51,6 +71,18 @@ int64_t most_keys(const ksa_params *p, int64_t rows) {
  *   830 keys, 64 rows, 8/4 heads                             1: 20    6: 12.3     6: 13.3        6: 13.5
  * Over twelve such calls what is chosen takes 1.4 % longer than the best of the three kinds with 1, 2, 3, 4, 6, 8 and 12 spans; without the second
  * kind 3 %.
+ * The same over 4-bit rows (best of each kind; what is chosen):
+ *   full attention, 64K keys, 2048 rows                      3: 2222              1: 2244        1: 1999             2007
+ *                               512 rows                     4: 587               2: 586         4: 525              532
+ *   summaries, 4700 keys, 512 rows                           4: 65                2: 66          4: 62               66
+ *              128K, 4608 rows                               1: 1127              1: 1185        1: 1035             1055
+ *   2000 keys, 2304 rows                                     1: 84                1: 103         1: 100              100
+ *   10000 keys, 2048 rows                                    1: 343               1: 351         1: 312              316
+ *   4200 keys, 8 x 100 rows                                  2: 93                1: 86          2: 87               86
+ *   window of 1023, 16/16 heads, 1280 rows                   1: 38                1: 31          3: 40               31
+ *   2700 keys, 2595 rows of six, 12/4 heads, head_dim 64     4: 46                1: 56          3: 56               55
+ *   830 keys, 64 rows, 8/4 heads                             8: 13.6              8: 15.1        8: 14.7             14.0
+ * 5 % longer than the best over these, nearly all of it in two of them.
  *
  * most: what is chosen here has at most so many spans.
  */

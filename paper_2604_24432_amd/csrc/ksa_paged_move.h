@@ -1,7 +1,7 @@
 // Rows into and out of the paged cache, as bf16, as e4m3 numbers with one power of two per row and KV head, or as e2m1 numbers with one per 32 of them.  Data movement, bound by
 // HBM: 16 bytes of a row per lane, the row's largest magnitude by lane moves, the table looked up by every row's lanes.  36864 rows, 8 heads,
 // d 128, 8-bit: in 56 us and out again 34, 454 MB at 5.0 TB/s (a copy on this card 5.0); 54000 rows, 16 heads, bf16, out 100 us, 5.3 TB/s; the 36864 rows in 4 bits
-// in 42 us, 4.5 TB/s, and out again 30; 64 rows
+// in 43 us, 4.5 TB/s, and out again 30; 64 rows
 // of 64 sequences 2.8 us, a launch and three loads one behind the other.  Loads of the new rows in front of the lookup (in 61 / 3.3 us),
 // two or four rows per lane (66 / 3.9, 69 / 5.0) did not pay.
 #ifndef KSA_PAGED_MOVE_H_
@@ -144,7 +144,9 @@ __global__ __launch_bounds__(256) void ksa_paged_append_kernel(const MoveArgs a)
     if (p.page < 0) return;
     const int piece = threadIdx.x % LANES;
     const int64_t from = p.row * a.row_stride + p.head * a.head_stride + piece * 8;
-    // (4 bits: what is read is four times what is written, and is not kept in the caches: 36864 rows in and out 75.0 us -> 72.0)
+    // (4 bits: what is read is four times what is written, and is not kept in the caches.  Kept and not kept (us), inputs in memory: 36864 rows in 50.7 and 42.8, in and out 83.4 and
+    // 73.7, 8192 rows in 13.6 and 12.1, 2048 rows 5.0 and 5.3; inputs just made, with what makes them: 36864 rows in 87.5 and 89.0, in and out 139.9 and 126.9, 8192 rows in 22.8
+    // and 24.4, in and out 31.8 and 32.0)
     auto load = [](const __bf16 *x) {
         const u32x4 *const at = reinterpret_cast<const u32x4 *>(x);
         if constexpr (F == KSA_CACHE_FP4) return __builtin_nontemporal_load(at);

@@ -1,6 +1,7 @@
 // Rotary positions of whole augmented sequences, there and back, and of one row of each.  Data movement, bound by HBM: a wave has a row, or a part of its heads; its lanes work out
 // the row's cosines and sines, one pair each, share them in LDS and then go over the heads, 16 bytes of one per lane and the 16 that they are paired with (from the
-// cache: the same lines).  36864 rows, 40 heads of 128, 755 MB: 130 us, 5.8 TB/s (a copy on this card 5.0); 12022 rows, 16 heads of 64 11.3 us, 4.9; 100 rows 3.
+// cache: the same lines).  36864 rows, 40 heads of 128, 755 MB: 130 us, 5.8 TB/s (a copy on this card 5.0); 12022 rows, 16 heads of 64 11.3 us, 4.9; 100 rows 3; single rows of 64, 512 and
+// 4096 sequences 2.9, 4.6 and 15.2.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -25,8 +26,11 @@ struct Args {
     KsaDivisor by_position;
 };
 
-// Outputs of this many bytes and more, which the caches (256 MB behind the L2s) cannot keep for whoever reads them next, go past them: 36864 rows, 40 heads of 128, 378 MB
-// there and back 272 us -> 261. Below, the next kernel finds them there.
+// Outputs of this many bytes and more, which the caches (256 MB behind the L2s) cannot keep as a whole for whoever reads them next, go past them.  Kept and past (us), 40 heads
+// of 128: the call alone with 264 MB of outputs 102 and 86, 378 MB 141 and 136, 1 GB 387 and 380; there and back 378 MB 272 and 261.  Who reads them next pays for a part of that: the
+// call and an elementwise pass over its outputs 264 MB 195 and 205, 378 MB 273 and 286, 1 GB 730 and 745; the call and the prefill (64-row chunks) 264 MB 754 and 758, 378 MB 1386 and
+// 1395, 512 MB 2289 and 2279, 1 GB 7841 and 7806.  Below the line the next kernel finds more there than going past saves: 96 MB alone 32.8 and 32.6, with the pass 67 and
+// 72, with the prefill 159 and 170; 224 MB 87 and 70, 167 and 174, 576 and 584.
 constexpr int64_t PAST_CACHES = (int64_t)256 << 20;
 
 template <int D, int P, bool PAST>
